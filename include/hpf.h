@@ -22,7 +22,8 @@
  *     its declaration): parameters, gradient buffers and the workspace belong
  *     to the caller, as do the streams.
  *   - Tensors are fp32, channels innermost: activations [n][h][w][c], conv
- *     weights [c_out][r][s][c_in].
+ *     weights [c_out][r][s][c_in].  Calls with a `dtype` argument take 16-bit
+ *     tensors too.
  *   - The step calls (forward, backward, grad_average) only enqueue work.
  *     hpf_loss and hpf_synchronize wait for it.
  *   - There is no CPU fallback: without a CUDA device the step calls fail with
@@ -352,6 +353,47 @@ int hpf_grad_average_flat(const float *d_slots, float *d_out, int32_t M, int64_t
 /* The same update on caller buffers: d_slots [M][G]; d_grad_avg [G] or NULL; d_params, d_velocity [G] updated in place. */
 int hpf_sgd_momentum_flat(const float *d_slots, float *d_grad_avg, float *d_params, float *d_velocity, int32_t M, int64_t G,
                           float lr, float momentum, float weight_decay, void *stream);
+
+/* ---- What logits are read for beyond the mean loss --------------------------------------------------------------
+ * d_logits [rows][classes] of type dtype, rows `ld` elements apart (any alignment the type has); 16-bit types are
+ * computed with in fp32.  A logit of -inf is a masked class: it has probability 0, is never listed and gets gradient 0.
+ * A row with nothing but -inf has no distribution (see each call).  A row with a NaN or +inf gives NaN.  A label
+ * outside [0, classes) is no label.  Statistics, losses and lists are fp32 / int32.  No workspace; a call is one
+ * kernel on `stream` of the current device, may be captured, and rows = 0 does nothing.  Results do not depend on timing. */
+typedef enum { HPF_FP32 = 0, HPF_BF16 = 1, HPF_FP16 = 2 } hpf_dtype;
+
+/* With s = logits / temperature:  d_lse = ln sum exp s;  d_logprob = s[label] - lse (0 without a label; -inf for a masked
+ * class or a row without a distribution);  d_entropy = lse - sum p s (0 without a distribution);  d_top_ids / d_top_logprobs
+ * [rows][k]: the k <= 64 largest classes, best first, equal logits by the lower class (places without a class: -1, -inf).
+ * Each output but the list (k = 0) may be NULL. */
+int hpf_logprobs_fwd(const void *d_logits, const int32_t *d_labels, float *d_logprob, float *d_entropy, float *d_lse,
+                     int32_t *d_top_ids, float *d_top_logprobs, int64_t rows, int32_t classes, int64_t ld, int32_t k,
+                     float temperature, int32_t dtype, void *stream);
+/* d_dlogits = (g (1[class = label] - p) - e p (ln p + entropy)) / temperature with g = d_dlogprob[row] (0 without a label),
+ * e = d_dentropy[row] (either may be NULL), lse and entropy as the forward call left them.  Rows with g = e = 0 and rows without a
+ * distribution get zeros, whatever they hold.  d_dlogits may be d_logits (with ld_d = ld). */
+int hpf_logprobs_bwd(const void *d_logits, const int32_t *d_labels, const float *d_lse, const float *d_entropy,
+                     const float *d_dlogprob, const float *d_dentropy, void *d_dlogits, int64_t rows, int32_t classes,
+                     int64_t ld, int64_t ld_d, float temperature, int32_t dtype, void *stream);
+
+/* Distillation from a teacher's list of k <= 256 classes per row (d_teacher_ids, d_teacher_logits: [rows][k]; log-probabilities
+ * serve as logits).  q = softmax(teacher / T) over the list, p_T = softmax(logits / T), p = softmax(logits):
+ *   loss[row] = alpha T^2 sum_j q_j (ln q_j - ln p_T[id_j]) + (1 - alpha) (-ln p[label])
+ * Entries outside [0, classes) or at -inf are not there; a list that holds nothing and a missing label drop their term; a class
+ * listed twice counts with both weights.  A masked class with q > 0 makes the loss +inf.  A row without a distribution has loss 0.
+ * d_labels may be NULL if alpha = 1.  d_stats [rows][2] is what the backward call needs (may be NULL). */
+int hpf_distill_fwd(const void *d_logits, const int32_t *d_labels, const int32_t *d_teacher_ids, const float *d_teacher_logits,
+                    float *d_loss, float *d_stats, int64_t rows, int32_t classes, int64_t ld, int32_t k, float temperature,
+                    float alpha, int32_t dtype, void *stream);
+/* d_dlogits = d_dloss[row] (alpha T (p_T - q) + (1 - alpha) (p - 1[class = label])).  Rows with a weight of 0 and rows without a
+ * distribution get zeros, whatever they hold.  d_dlogits may be d_logits (with ld_d = ld). */
+int hpf_distill_bwd(const void *d_logits, const int32_t *d_labels, const int32_t *d_teacher_ids, const float *d_teacher_logits,
+                    const float *d_stats, const float *d_dloss, void *d_dlogits, int64_t rows, int32_t classes, int64_t ld,
+                    int64_t ld_d, int32_t k, float temperature, float alpha, int32_t dtype, void *stream);
+/* Both in one kernel, which reads the logits from memory once. */
+int hpf_distill_fwd_bwd(const void *d_logits, const int32_t *d_labels, const int32_t *d_teacher_ids, const float *d_teacher_logits,
+                        const float *d_dloss, float *d_loss, void *d_dlogits, int64_t rows, int32_t classes, int64_t ld,
+                        int64_t ld_d, int32_t k, float temperature, float alpha, int32_t dtype, void *stream);
 
 const char *hpf_strerror(int status);
 /* Text of the most recent failure on the calling thread (CUDA error string and call site). */

@@ -7,6 +7,9 @@ from . import build as _build
 CONV, BNRELU, ADD, MAXPOOL, HEAD, BN, RELU = 1, 2, 3, 4, 5, 6, 7
 OPT_GRAPH, OPT_CONV_PATH, OPT_SINGLE_STREAM, OPT_KEEP_MESSAGES, OPT_FUSE_ADD, OPT_PDL, OPT_WGRAD_PASSES, OPT_FUSE_BN, OPT_CELL_TIMES, OPT_BN_CLUSTER, OPT_CELL_CTAS, OPT_PDL_LATE_FROM, OPT_STAGE_LANES, OPT_WGRAD_DIRECT, OPT_GROUP_LAUNCHES = 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15
 
+FP32, BF16, FP16 = 0, 1, 2
+ERR_INVALID, ERR_UNSUPPORTED = -1, -2
+
 
 class HpfError(RuntimeError):
     def __init__(self, status, text):
@@ -80,6 +83,11 @@ _SIGNATURES = {
     "hpf_grad_average_flat": [_vp, _vp, _i32, _i64, _vp],
     "hpf_bnrelu_fwd_static": [_vp, _vp, _vp, _f32, _vp, _vp, _i64, _i32, _vp],
     "hpf_static_scratch_bytes": [C.POINTER(C.c_size_t)],
+    "hpf_logprobs_fwd": [_vp] * 7 + [_i64, _i32, _i64, _i32, _f32, _i32, _vp],
+    "hpf_logprobs_bwd": [_vp] * 7 + [_i64, _i32, _i64, _i64, _f32, _i32, _vp],
+    "hpf_distill_fwd": [_vp] * 6 + [_i64, _i32, _i64, _i32, _f32, _f32, _i32, _vp],
+    "hpf_distill_bwd": [_vp] * 7 + [_i64, _i32, _i64, _i64, _i32, _f32, _f32, _i32, _vp],
+    "hpf_distill_fwd_bwd": [_vp] * 7 + [_i64, _i32, _i64, _i64, _i32, _f32, _f32, _i32, _vp],
 }
 EXPORTS = sorted(list(_SIGNATURES) + ["hpf_strerror", "hpf_last_error"])
 
@@ -122,6 +130,39 @@ def _stream(stream):
         import torch
         return torch.cuda.current_stream().cuda_stream
     return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+_dtypes = {}
+
+
+def _dtype_of(t, what):
+    """FP32 / BF16 / FP16 of a torch tensor."""
+    if not _dtypes:
+        import torch
+        _dtypes.update({torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16})
+    d = _dtypes.get(t.dtype)
+    if d is None:
+        raise HpfError(ERR_INVALID, f"{what}: fp32, bf16 or fp16 is wanted, got {t.dtype}")
+    return d
+
+
+def _ptrs(stream, *named):
+    """Device pointers of (name, tensor or None, torch dtype) and the stream's handle.  A tensor of another type, on the host or on
+    another device than the current one is refused: the kernel would read it wrongly or not at all."""
+    import torch
+    device = torch.cuda.current_device()
+    out = []
+    for name, t, dtype in named:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype != dtype:
+            raise HpfError(ERR_INVALID, f"{name}: {dtype} is wanted, got {t.dtype}")
+        if t.get_device() != device:
+            raise HpfError(ERR_INVALID, f"{name} is on {t.device}, the current device is cuda:{device}")
+        out.append(t.data_ptr())
+    out.append(torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    return out
 
 
 def _op_array(ops):
@@ -358,3 +399,54 @@ def bnrelu_fwd_static(x, gamma, beta, eps, y, stats, rows, Cc, stream=None):
 
 def static_scratch_bytes():
     n = C.c_size_t(); _check(lib().hpf_static_scratch_bytes(C.byref(n))); return n.value
+
+
+# ---- label log-probabilities and distillation: logits [rows][classes] in fp32, bf16 or fp16, rows `ld` elements apart --------
+def logprobs_fwd(logits, labels, logprob, entropy, lse, top_ids, top_logprobs, rows, classes, ld, k=0, temperature=1.0, stream=None):
+    """Log-probability of each row's label, entropy, log-sum-exp and the k likeliest classes (see hpf.h); outputs may be None."""
+    import torch
+    f, i = torch.float32, torch.int32
+    dt = _dtype_of(logits, "logits")
+    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("logprob", logprob, f), ("entropy", entropy, f),
+                   ("lse", lse, f), ("top_ids", top_ids, i), ("top_logprobs", top_logprobs, f))
+    _check(lib().hpf_logprobs_fwd(*p, rows, classes, ld, k, temperature, dt, st))
+
+
+def logprobs_bwd(logits, labels, lse, entropy, d_logprob, d_entropy, d_logits, rows, classes, ld, ld_d, temperature=1.0, stream=None):
+    """Gradient of log-probability and entropy; d_logits may be logits."""
+    import torch
+    f = torch.float32
+    dt = _dtype_of(logits, "logits")
+    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, torch.int32), ("lse", lse, f), ("entropy", entropy, f),
+                   ("d_logprob", d_logprob, f), ("d_entropy", d_entropy, f), ("d_logits", d_logits, logits.dtype))
+    _check(lib().hpf_logprobs_bwd(*p, rows, classes, ld, ld_d, temperature, dt, st))
+
+
+def distill_fwd(logits, labels, teacher_ids, teacher_logits, loss, stats, rows, classes, ld, k, temperature=1.0, alpha=1.0, stream=None):
+    """Loss per row against a teacher's k listed logits, mixed with cross-entropy on the labels (see hpf.h)."""
+    import torch
+    f, i = torch.float32, torch.int32
+    dt = _dtype_of(logits, "logits")
+    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("teacher_ids", teacher_ids, i),
+                   ("teacher_logits", teacher_logits, f), ("loss", loss, f), ("stats", stats, f))
+    _check(lib().hpf_distill_fwd(*p, rows, classes, ld, k, temperature, alpha, dt, st))
+
+
+def distill_bwd(logits, labels, teacher_ids, teacher_logits, stats, d_loss, d_logits, rows, classes, ld, ld_d, k, temperature=1.0, alpha=1.0, stream=None):
+    """Its gradient from the statistics that distill_fwd left; d_logits may be logits."""
+    import torch
+    f, i = torch.float32, torch.int32
+    dt = _dtype_of(logits, "logits")
+    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("teacher_ids", teacher_ids, i),
+                   ("teacher_logits", teacher_logits, f), ("stats", stats, f), ("d_loss", d_loss, f), ("d_logits", d_logits, logits.dtype))
+    _check(lib().hpf_distill_bwd(*p, rows, classes, ld, ld_d, k, temperature, alpha, dt, st))
+
+
+def distill_fwd_bwd(logits, labels, teacher_ids, teacher_logits, d_loss, loss, d_logits, rows, classes, ld, ld_d, k, temperature=1.0, alpha=1.0, stream=None):
+    """Loss and gradient in one kernel."""
+    import torch
+    f, i = torch.float32, torch.int32
+    dt = _dtype_of(logits, "logits")
+    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("teacher_ids", teacher_ids, i),
+                   ("teacher_logits", teacher_logits, f), ("d_loss", d_loss, f), ("loss", loss, f), ("d_logits", d_logits, logits.dtype))
+    _check(lib().hpf_distill_fwd_bwd(*p, rows, classes, ld, ld_d, k, temperature, alpha, dt, st))
