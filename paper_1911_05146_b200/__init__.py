@@ -8,4 +8,5 @@ from .binding import (HpfError, Model, lib, estimate_op_costs, balance_cuts, CON
                       conv_fwd, conv_dgrad, conv_wgrad, conv_prepare_weights, conv_scratch_bytes,
                       bnrelu_fwd, bnrelu_bwd, bnrelu_scratch_bytes, bnrelu_status, grad_average_flat, sgd_momentum_flat,
                       bnrelu_fwd_static, static_scratch_bytes, FP32, BF16, FP16,
+                      ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, linear_scratch_bytes, linear_fwd, linear_bwd, linear_status,
                       logprobs_fwd, logprobs_bwd, distill_fwd, distill_bwd, distill_fwd_bwd)

@@ -8,6 +8,7 @@ CONV, BNRELU, ADD, MAXPOOL, HEAD, BN, RELU = 1, 2, 3, 4, 5, 6, 7
 OPT_GRAPH, OPT_CONV_PATH, OPT_SINGLE_STREAM, OPT_KEEP_MESSAGES, OPT_FUSE_ADD, OPT_PDL, OPT_WGRAD_PASSES, OPT_FUSE_BN, OPT_CELL_TIMES, OPT_BN_CLUSTER, OPT_CELL_CTAS, OPT_PDL_LATE_FROM, OPT_STAGE_LANES, OPT_WGRAD_DIRECT, OPT_GROUP_LAUNCHES = 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15
 
 FP32, BF16, FP16 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 ERR_INVALID, ERR_UNSUPPORTED = -1, -2
 
 
@@ -83,6 +84,10 @@ _SIGNATURES = {
     "hpf_grad_average_flat": [_vp, _vp, _i32, _i64, _vp],
     "hpf_bnrelu_fwd_static": [_vp, _vp, _vp, _f32, _vp, _vp, _i64, _i32, _vp],
     "hpf_static_scratch_bytes": [C.POINTER(C.c_size_t)],
+    "hpf_linear_scratch_bytes": [_i64, _i32, _i32, _i64, _i64, _i32, _i32, _i32, C.POINTER(C.c_size_t)],
+    "hpf_linear_fwd": [_vp] * 6 + [_i64, _i32, _i32, _i64, _i64, _i32, _i32, _vp, C.c_size_t, _vp],
+    "hpf_linear_bwd": [_vp] * 7 + [_i64, _i32, _i32, _i64, _i64, _i32, _i32, _i32, _vp, C.c_size_t, _vp],
+    "hpf_linear_status": [_vp, _pi32],
     "hpf_logprobs_fwd": [_vp] * 7 + [_i64, _i32, _i64, _i32, _f32, _i32, _vp],
     "hpf_logprobs_bwd": [_vp] * 7 + [_i64, _i32, _i64, _i64, _f32, _i32, _vp],
     "hpf_distill_fwd": [_vp] * 6 + [_i64, _i32, _i64, _i32, _f32, _f32, _i32, _vp],
@@ -135,14 +140,14 @@ def _stream(stream):
 _dtypes = {}
 
 
-def _dtype_of(t, what):
-    """FP32 / BF16 / FP16 of a torch tensor."""
+def _dtype_of(dtype, what):
+    """FP32 / BF16 / FP16 of a torch dtype."""
     if not _dtypes:
         import torch
         _dtypes.update({torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16})
-    d = _dtypes.get(t.dtype)
+    d = _dtypes.get(dtype)
     if d is None:
-        raise HpfError(ERR_INVALID, f"{what}: fp32, bf16 or fp16 is wanted, got {t.dtype}")
+        raise HpfError(ERR_INVALID, f"{what}: fp32, bf16 or fp16 is wanted, got {dtype}")
     return d
 
 
@@ -401,12 +406,43 @@ def static_scratch_bytes():
     n = C.c_size_t(); _check(lib().hpf_static_scratch_bytes(C.byref(n))); return n.value
 
 
+# ---- the linear layer: x [rows][n_in] and W [n_out][n_in] in fp32, bf16 or fp16, rows of x and dx ld_x, of the rest ld_y elements apart ----
+def linear_scratch_bytes(rows, n_in, n_out, ld_x, ld_y, dtype, act=ACT_NONE, aligned=True):
+    """Bytes of scratch for both directions; dtype is a torch dtype, aligned: every tensor starts on a 16-byte boundary."""
+    n = C.c_size_t(); _check(lib().hpf_linear_scratch_bytes(rows, n_in, n_out, ld_x, ld_y, _dtype_of(dtype, "dtype"), act, int(aligned), C.byref(n)))
+    return n.value
+
+
+def linear_fwd(x, w, bias, residual, y, z, rows, n_in, n_out, ld_x, ld_y, act, scratch, stream=None):
+    """y = act(x W^T + bias) + residual; bias, residual and z (what the activation is applied to) may be None (see hpf.h)."""
+    import torch
+    t = x.dtype
+    dt = _dtype_of(t, "x")
+    *p, ws, st = _ptrs(stream, ("x", x, t), ("w", w, t), ("bias", bias, t), ("residual", residual, t), ("y", y, t), ("z", z, t), ("scratch", scratch, torch.uint8))
+    _check(lib().hpf_linear_fwd(*p, rows, n_in, n_out, ld_x, ld_y, dt, act, ws, scratch.numel(), st))
+
+
+def linear_bwd(dy, z, x, w, dx, dw, dbias, rows, n_in, n_out, ld_x, ld_y, act, scratch, stream=None):
+    """Gradients of linear_fwd, each None if not wanted; dw and dbias may be fp32 whatever the rest is."""
+    import torch
+    t = dy.dtype
+    dt = _dtype_of(t, "dy")
+    g = dw.dtype if dw is not None else dbias.dtype if dbias is not None else t
+    *p, ws, st = _ptrs(stream, ("dy", dy, t), ("z", z, t), ("x", x, t), ("w", w, t), ("dx", dx, t), ("dw", dw, g), ("dbias", dbias, g), ("scratch", scratch, torch.uint8))
+    _check(lib().hpf_linear_bwd(*p, rows, n_in, n_out, ld_x, ld_y, dt, act, _dtype_of(g, "dw"), ws, scratch.numel(), st))
+
+
+def linear_status(scratch):
+    """True if a bounded wait of a linear call on this scratch gave up (the scratch head must then be zeroed again)."""
+    v = _i32(); _check(lib().hpf_linear_status(_ptr(scratch), C.byref(v))); return bool(v.value)
+
+
 # ---- label log-probabilities and distillation: logits [rows][classes] in fp32, bf16 or fp16, rows `ld` elements apart --------
 def logprobs_fwd(logits, labels, logprob, entropy, lse, top_ids, top_logprobs, rows, classes, ld, k=0, temperature=1.0, stream=None):
     """Log-probability of each row's label, entropy, log-sum-exp and the k likeliest classes (see hpf.h); outputs may be None."""
     import torch
     f, i = torch.float32, torch.int32
-    dt = _dtype_of(logits, "logits")
+    dt = _dtype_of(logits.dtype, "logits")
     *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("logprob", logprob, f), ("entropy", entropy, f),
                    ("lse", lse, f), ("top_ids", top_ids, i), ("top_logprobs", top_logprobs, f))
     _check(lib().hpf_logprobs_fwd(*p, rows, classes, ld, k, temperature, dt, st))
@@ -416,7 +452,7 @@ def logprobs_bwd(logits, labels, lse, entropy, d_logprob, d_entropy, d_logits, r
     """Gradient of log-probability and entropy; d_logits may be logits."""
     import torch
     f = torch.float32
-    dt = _dtype_of(logits, "logits")
+    dt = _dtype_of(logits.dtype, "logits")
     *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, torch.int32), ("lse", lse, f), ("entropy", entropy, f),
                    ("d_logprob", d_logprob, f), ("d_entropy", d_entropy, f), ("d_logits", d_logits, logits.dtype))
     _check(lib().hpf_logprobs_bwd(*p, rows, classes, ld, ld_d, temperature, dt, st))
@@ -426,7 +462,7 @@ def distill_fwd(logits, labels, teacher_ids, teacher_logits, loss, stats, rows, 
     """Loss per row against a teacher's k listed logits, mixed with cross-entropy on the labels (see hpf.h)."""
     import torch
     f, i = torch.float32, torch.int32
-    dt = _dtype_of(logits, "logits")
+    dt = _dtype_of(logits.dtype, "logits")
     *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("teacher_ids", teacher_ids, i),
                    ("teacher_logits", teacher_logits, f), ("loss", loss, f), ("stats", stats, f))
     _check(lib().hpf_distill_fwd(*p, rows, classes, ld, k, temperature, alpha, dt, st))
@@ -436,7 +472,7 @@ def distill_bwd(logits, labels, teacher_ids, teacher_logits, stats, d_loss, d_lo
     """Its gradient from the statistics that distill_fwd left; d_logits may be logits."""
     import torch
     f, i = torch.float32, torch.int32
-    dt = _dtype_of(logits, "logits")
+    dt = _dtype_of(logits.dtype, "logits")
     *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("teacher_ids", teacher_ids, i),
                    ("teacher_logits", teacher_logits, f), ("stats", stats, f), ("d_loss", d_loss, f), ("d_logits", d_logits, logits.dtype))
     _check(lib().hpf_distill_bwd(*p, rows, classes, ld, ld_d, k, temperature, alpha, dt, st))
@@ -446,7 +482,7 @@ def distill_fwd_bwd(logits, labels, teacher_ids, teacher_logits, d_loss, loss, d
     """Loss and gradient in one kernel."""
     import torch
     f, i = torch.float32, torch.int32
-    dt = _dtype_of(logits, "logits")
+    dt = _dtype_of(logits.dtype, "logits")
     *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("teacher_ids", teacher_ids, i),
                    ("teacher_logits", teacher_logits, f), ("d_loss", d_loss, f), ("loss", loss, f), ("d_logits", d_logits, logits.dtype))
     _check(lib().hpf_distill_fwd_bwd(*p, rows, classes, ld, ld_d, k, temperature, alpha, dt, st))

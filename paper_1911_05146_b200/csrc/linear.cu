@@ -1,0 +1,892 @@
+// The linear layer: y = act(x W^T + b) + residual, and its gradients (hpf_linear_fwd, hpf_linear_bwd).
+//
+// Three matrix products share one kernel, out[M][N] = sum_k A(m, k) B(n, k), because an operand may be read either way round:
+//   forward  out = y [rows][out]   A = x  (k contiguous)           B = W (k contiguous)
+//   dx       out = dx [rows][in]   A = dz (k = out contiguous)     B = W (n = in contiguous)
+//   dW       out = dW [out][in]    A = dz (m = out contiguous)     B = x (n = in contiguous)
+// dz = dy * act'(z) and db = sum_rows dz come from a kernel of their own ahead of the two, since both products read dz.
+//
+// One CTA per SM: a TMA producer, one thread issuing tcgen05.mma into TMEM (two accumulators, so that the write-out of a tile runs
+// under the next one's products) and eight write-out warps.  A tile is 128 x BN; a stage of the ring is 128 bytes of k.
+// 16-bit operands: one MMA per 16 k, fp32 accumulators.  fp32 operands: x = hi + lo with hi the bits a TF32 operand keeps; four more
+// warps write lo beside each stage and three MMAs form hi hi + lo hi + hi lo.  What is left out of a product (lo lo, and the bits of a lo
+// that TF32 drops) is below 3 2^-20 of it, about 2^-21 on average.
+// The accumulator truncates each addition, an error that grows with the number of additions and always points to zero: where the
+// result is fp32, sums are taken out of TMEM every kChunk stages and added up in registers, rounded to nearest.
+//
+// Few tiles (few rows, small layers): the k loop is split over a cluster of up to 8 CTAs.  Each leaves its fp32 partial tile in
+// its own shared memory; the CTAs then add the partial tiles up over distributed shared memory, always in rank order.
+#include "../../include/hpf.h"
+#include "conv_tc.h"
+#include "hpf_kernels.h"
+#include "tc_ptx.cuh"
+
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <math.h>
+
+namespace cg = cooperative_groups;
+
+namespace hpf {
+namespace {
+
+constexpr int kRow = 128;                      // bytes of k (or of m / n) in a row of a stage: the swizzle's width
+constexpr int kRing = 192 * 1024;              // bytes of the ring of stages
+constexpr int kBlock = 4096;                   // a 32 x 32 block of fp32 on its way out
+constexpr int kOutWarps = 8;
+constexpr int kSmem = kRing + kOutWarps * kBlock + 1024 + 512;
+constexpr int kChunk = 4;                      // stages whose products are added up in TMEM where the result is fp32
+constexpr int kMaxSplit = 8;
+
+struct GemmArgs {
+    CUtensorMap ta, tb;
+    int M, N, k_blocks, tiles_m, tiles_n, split;
+    int a_mn, b_mn;                            // operand has m / n contiguous (else k)
+    uint32_t idesc;
+    int act, wide;                             // wide: every output and the residual take 16-byte accesses
+    void *out, *z;
+    const void *bias, *residual;
+    int64_t ld;                                // of out, z and residual
+    DeviceStatus* status;
+};
+
+// ---- PTX this kernel adds ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "}\n" ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// 32 lanes x 32 consecutive 32-bit columns, arrived: thread i of the warp receives lane (base lane + i)
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v)
+{
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+        "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+// A wait that does not look at the abort flag: for copies in flight after another wait gave up.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity)
+{
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitLimit) {}
+}
+// Operand with m / n contiguous, 16-bit: rows of 64 values (128 bytes, 128-byte swizzle), 8 rows of k 1024 bytes apart, the next
+// 64 values of m / n `block_bytes` further on.
+__device__ __forceinline__ uint64_t desc_mn16(uint32_t addr, uint32_t block_bytes) { return smem_desc(addr, block_bytes, 1024, 128); }
+
+// ---- element types ----------------------------------------------------------------------------------------------------
+template <typename T> struct Pack;
+template <> struct Pack<float> {
+    static constexpr int V = 4;
+    static __device__ __forceinline__ void unpack(const uint4& r, float* f)
+    {
+        f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float* f)
+    {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+    static __device__ __forceinline__ float get(float v) { return v; }
+    static __device__ __forceinline__ float put(float v) { return v; }
+};
+template <> struct Pack<__nv_bfloat16> {
+    static constexpr int V = 8;
+    static __device__ __forceinline__ void unpack(const uint4& r, float* f)
+    {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ uint32_t two(float a, float b)
+    {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ uint4 pack(const float* f) { return make_uint4(two(f[0], f[1]), two(f[2], f[3]), two(f[4], f[5]), two(f[6], f[7])); }
+    static __device__ __forceinline__ float get(__nv_bfloat16 v) { return __bfloat162float(v); }
+    static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
+};
+template <> struct Pack<__half> {
+    static constexpr int V = 8;
+    static __device__ __forceinline__ void unpack(const uint4& r, float* f)
+    {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            f[2 * i] = v.x; f[2 * i + 1] = v.y;
+        }
+    }
+    static __device__ __forceinline__ uint32_t two(float a, float b)
+    {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ uint4 pack(const float* f) { return make_uint4(two(f[0], f[1]), two(f[2], f[3]), two(f[4], f[5]), two(f[6], f[7])); }
+    static __device__ __forceinline__ float get(__half v) { return __half2float(v); }
+    static __device__ __forceinline__ __half put(float v) { return __float2half_rn(v); }
+};
+
+// gelu is z Phi(z) with the error function, silu z / (1 + e^-z)
+__device__ __forceinline__ float activate(float z, int act)
+{
+    if (act == HPF_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
+    if (act == HPF_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678f));
+    if (act == HPF_ACT_SILU) return z / (1.f + expf(-z));
+    return z;
+}
+__device__ __forceinline__ float slope(float z, int act)
+{
+    if (act == HPF_ACT_RELU) return z > 0.f ? 1.f : (z != z ? z : 0.f);
+    if (act == HPF_ACT_GELU) return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
+    if (act == HPF_ACT_SILU) {
+        const float s = 1.f / (1.f + expf(-z));
+        return s * fmaf(z, 1.f - s, 1.f);
+    }
+    return 1.f;
+}
+
+// ---- the product ------------------------------------------------------------------------------------------------------
+struct Tile {
+    int m, n;
+};
+// Tiles in groups of 16 rows of tiles, so that CTAs working at the same time share operands in L2.
+__device__ __forceinline__ Tile tile_at(int t, int tiles_m, int tiles_n)
+{
+    constexpr int G = 16;
+    const int group = t / (G * tiles_n), first = group * G;
+    const int rows = min(tiles_m - first, G), in = t - group * G * tiles_n;
+    return Tile{first + in % rows, in / rows};
+}
+// Where 16-byte unit u of row r of a 32 x 32 block lies: units of a row are spread so that both the writers (a row per lane) and the
+// readers (a few rows at a time) touch all banks.
+__device__ __forceinline__ uint32_t unit_at(uint32_t block, int r, int u) { return block + r * 128 + ((u ^ (r & 7)) << 4); }
+__device__ __forceinline__ void block_put(uint32_t block, int lane, const float* v)
+{
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(unit_at(block, lane, u)), "f"(v[4 * u]), "f"(v[4 * u + 1]), "f"(v[4 * u + 2]), "f"(v[4 * u + 3])
+                     : "memory");
+}
+__device__ __forceinline__ float4 shared_get(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 cluster_get(uint32_t addr, int rank)
+{
+    float4 v;
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
+    return v;
+}
+
+// One warp finishes the 32 x 32 block whose fp32 sums lie in shared memory (of `split` CTAs, added up in rank order): bias,
+// activation, residual, one rounding.  A lane holds 16 bytes of a row, so every access to memory is whole sectors.
+template <typename T>
+__device__ __forceinline__ void finish_block(const GemmArgs& p, uint32_t block, int split, int row0, int col0, int lane)
+{
+    constexpr int V = Pack<T>::V, PER_ROW = 32 / V, ROWS = 32 / PER_ROW;
+    const int col = col0 + (lane % PER_ROW) * V;
+    if (row0 >= p.M || col >= p.N) return;
+    const bool wide = p.wide && col + V <= p.N;
+    float bias[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) bias[j] = p.bias && col + j < p.N ? Pack<T>::get(reinterpret_cast<const T*>(p.bias)[col + j]) : 0.f;
+#pragma unroll
+    for (int i = 0; i < PER_ROW; ++i) {
+        const int r = i * ROWS + lane / PER_ROW, row = row0 + r;
+        if (row >= p.M) continue;
+        float v[V];
+#pragma unroll
+        for (int h = 0; h < V / 4; ++h) {
+            const uint32_t at = unit_at(block, r, (lane % PER_ROW) * (V / 4) + h);
+            float4 s = split == 1 ? shared_get(at) : cluster_get(at, 0);
+            for (int k = 1; k < split; ++k) {
+                const float4 o = cluster_get(at, k);
+                s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+            }
+            v[4 * h] = s.x; v[4 * h + 1] = s.y; v[4 * h + 2] = s.z; v[4 * h + 3] = s.w;
+        }
+        const int64_t at = row * p.ld + col;
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] += bias[j];
+        if (p.z) {
+            T* z = reinterpret_cast<T*>(p.z) + at;
+            if (wide) *reinterpret_cast<uint4*>(z) = Pack<T>::pack(v);
+            else
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (col + j < p.N) z[j] = Pack<T>::put(v[j]);
+        }
+        if (p.act != HPF_ACT_NONE) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = activate(v[j], p.act);
+        }
+        if (p.residual) {
+            const T* res = reinterpret_cast<const T*>(p.residual) + at;
+            float f[V];
+            if (wide) Pack<T>::unpack(*reinterpret_cast<const uint4*>(res), f);
+            else
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[j] = col + j < p.N ? Pack<T>::get(res[j]) : 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] += f[j];
+        }
+        T* out = reinterpret_cast<T*>(p.out) + at;
+        if (wide) *reinterpret_cast<uint4*>(out) = Pack<T>::pack(v);
+        else
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (col + j < p.N) out[j] = Pack<T>::put(v[j]);
+    }
+}
+
+// E: bytes of an operand value (2: fp16 / bf16, 4: fp32 as three TF32 products).  PROMOTE: sums leave TMEM every kChunk stages.
+template <int E, int BN>
+struct Shape {
+    static constexpr int kA = kTileM * kRow, kB = BN * kRow;
+    static constexpr int kStage = (kA + kB) * (E == 4 ? 2 : 1);
+    static constexpr int kStages = kRing / kStage;
+    static constexpr int kThreads = (4 + kOutWarps + (E == 4 ? 4 : 0)) * 32;
+    static constexpr int kInner = kRow / E;              // values in a row of a stage
+};
+
+template <int E, typename T, int BN, bool PROMOTE>
+__global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(const __grid_constant__ GemmArgs p)
+{
+    using S = Shape<E, BN>;
+    constexpr int STAGES = S::kStages;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) unsigned long long s_bars[3 * 8 + 4];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t staging = ring + kRing;
+    const uint32_t full = smem_u32(s_bars), empty = full + 64, ready = full + 128, acc_full = full + 192, acc_empty = acc_full + 16;
+    const int warp = warp_index(), lane = threadIdx.x & 31;
+    const int split = p.split;
+    const int rank = split > 1 ? (int)(blockIdx.x % (unsigned)split) : 0;
+    const int tiles = p.tiles_m * p.tiles_n;
+    const int first = (int)(blockIdx.x / (unsigned)split), step = split > 1 ? tiles : (int)gridDim.x;      // a cluster has one tile
+    const int kb0 = (int)((long long)p.k_blocks * rank / split), kb1 = (int)((long long)p.k_blocks * (rank + 1) / split);
+
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        for (int i = 0; i < STAGES; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+            mbar_init(ready + 8 * i, 4);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(acc_full + 8 * i, 1);
+            mbar_init(acc_empty + 8 * i, kOutWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) tmem_alloc(smem_u32(&s_tmem), 2 * BN);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    volatile int* abort_flag = &s_abort;
+
+    if (warp == 0) {
+        if (elect_one()) {
+            prefetch_tmap(&p.ta);
+            prefetch_tmap(&p.tb);
+            int it = 0;
+            bool live = true;
+            for (int t = first; live && t < tiles; t += step) {
+                const Tile tile = tile_at(t, p.tiles_m, p.tiles_n);
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const int s = it % STAGES;
+                    if (!mbar_wait(empty + 8 * s, ((it / STAGES) & 1) ^ 1, abort_flag)) { report(p.status, 40); live = false; break; }
+                    const uint32_t a = ring + s * S::kStage, b = a + S::kA, bar = full + 8 * s;
+                    mbar_expect_tx(bar, S::kA + S::kB);
+                    const int k = kb * S::kInner;
+                    if (p.a_mn) {
+#pragma unroll
+                        for (int i = 0; i < kTileM / S::kInner; ++i) tma_load_2d(a + i * S::kInner * kRow, &p.ta, bar, tile.m * kTileM + i * S::kInner, k);
+                    } else {
+                        tma_load_2d(a, &p.ta, bar, k, tile.m * kTileM);
+                    }
+                    if (p.b_mn) {
+#pragma unroll
+                        for (int i = 0; i < BN / S::kInner; ++i) tma_load_2d(b + i * S::kInner * kRow, &p.tb, bar, tile.n * BN + i * S::kInner, k);
+                    } else {
+                        tma_load_2d(b, &p.tb, bar, k, tile.n * BN);
+                    }
+                }
+            }
+            // nothing leaves while a copy is in flight: the last copies into each stage have landed when its full barrier has turned
+            for (int i = it > STAGES ? it - STAGES : 0; i < it; ++i) mbar_drain(full + 8 * (i % STAGES), (i / STAGES) & 1);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (elect_one()) {
+            const uint64_t layout_step_a = p.a_mn ? (E == 4 ? 1024 >> 4 : 2048 >> 4) : 2;
+            const uint64_t layout_step_b = p.b_mn ? (E == 4 ? 1024 >> 4 : 2048 >> 4) : 2;
+            int it = 0, chunk = 0;
+            bool live = true;
+            for (int t = first; live && t < tiles; t += step) {
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const int in_chunk = PROMOTE ? (kb - kb0) % kChunk : kb - kb0;
+                    const int buf = chunk & 1;
+                    if (in_chunk == 0) {
+                        if (!mbar_wait(acc_empty + 8 * buf, ((chunk >> 1) & 1) ^ 1, abort_flag)) { report(p.status, 41); live = false; break; }
+                        tc_fence_after();
+                    }
+                    const int s = it % STAGES;
+                    if (!mbar_wait((E == 4 ? ready : full) + 8 * s, (it / STAGES) & 1, abort_flag)) { report(p.status, 42); live = false; break; }
+                    tc_fence_after();
+                    const uint32_t a = ring + s * S::kStage, b = a + S::kA;
+                    uint64_t da, db;
+                    if (E == 4) {
+                        da = p.a_mn ? smem_desc_mn(a, S::kInner * kRow) : smem_desc(a, 16, 1024, 128);
+                        db = p.b_mn ? smem_desc_mn(b, S::kInner * kRow) : smem_desc(b, 16, 1024, 128);
+                    } else {
+                        da = p.a_mn ? desc_mn16(a, S::kInner * kRow) : smem_desc(a, 16, 1024, 128);
+                        db = p.b_mn ? desc_mn16(b, S::kInner * kRow) : smem_desc(b, 16, 1024, 128);
+                    }
+                    const uint32_t d = tmem + buf * BN;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint64_t ak = da + k * layout_step_a, bk = db + k * layout_step_b;
+                        const uint32_t more = in_chunk > 0 || k > 0;
+                        if constexpr (E == 4) {
+                            constexpr uint64_t lo = (uint64_t)(S::kA + S::kB) >> 4;
+                            umma_tf32(d, ak + lo, bk, p.idesc, more);
+                            umma_tf32(d, ak, bk + lo, p.idesc, 1);
+                            umma_tf32(d, ak, bk, p.idesc, 1);
+                        } else {
+                            umma_f16(d, ak, bk, p.idesc, more);
+                        }
+                    }
+                    umma_commit(empty + 8 * s);
+                    if (kb + 1 == kb1 || (PROMOTE && in_chunk + 1 == kChunk)) {
+                        umma_commit(acc_full + 8 * buf);
+                        ++chunk;
+                    }
+                }
+            }
+            // the products issued have read their stages when the last commits of these have arrived
+            for (int i = it > STAGES ? it - STAGES : 0; i < it; ++i) mbar_drain(empty + 8 * (i % STAGES), (i / STAGES) & 1);
+        }
+        __syncwarp();
+    } else if (warp >= 4 && warp < 4 + kOutWarps) {
+        const int quad = warp & 3, half = (warp - 4) >> 2;
+        constexpr int BLOCKS = BN / 64;                       // blocks of 32 columns of this warp
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        const uint32_t mine = staging + (warp - 4) * kBlock;
+        int chunk = 0;
+        bool live = true;
+        for (int t = first; live && t < tiles; t += step) {
+            const Tile tile = tile_at(t, p.tiles_m, p.tiles_n);
+            const int row0 = tile.m * kTileM + quad * 32;
+            if constexpr (PROMOTE) {
+                float acc[BLOCKS][32];
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) acc[b][j] = 0.f;
+                for (int kb = kb0; live && kb < kb1; kb += kChunk, ++chunk) {
+                    const int buf = chunk & 1;
+                    live = mbar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, abort_flag);
+                    live = __all_sync(0xffffffffu, live);
+                    if (!live) { report(p.status, 43); break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b) {
+                        float v[32];
+                        const uint32_t at = tmem + lanes + buf * BN + (half * BLOCKS + b) * 32;
+                        tmem_ld32(at, v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) acc[b][j] += v[j];
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
+                }
+                if (!live) break;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    const int c = half * BLOCKS + b;
+                    if (split > 1) {
+                        block_put(ring + (c * 4 + quad) * kBlock, lane, acc[b]);
+                    } else {
+                        block_put(mine, lane, acc[b]);
+                        __syncwarp();
+                        finish_block<T>(p, mine, 1, row0, tile.n * BN + c * 32, lane);
+                        __syncwarp();
+                    }
+                }
+            } else {
+                const int buf = chunk & 1;
+                live = mbar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, abort_flag);
+                live = __all_sync(0xffffffffu, live);
+                if (!live) { report(p.status, 43); break; }
+                tc_fence_after();
+                ++chunk;
+#pragma unroll 1
+                for (int b = 0; b < BLOCKS; ++b) {
+                    const int c = half * BLOCKS + b;
+                    float v[32];
+                    const uint32_t at = tmem + lanes + buf * BN + c * 32;
+                    tmem_ld32(at, v);
+                    if (b == BLOCKS - 1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
+                    }
+                    if (split > 1) {
+                        block_put(ring + (c * 4 + quad) * kBlock, lane, v);
+                    } else {
+                        block_put(mine, lane, v);
+                        __syncwarp();
+                        finish_block<T>(p, mine, 1, row0, tile.n * BN + c * 32, lane);
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+    } else if (E == 4 && warp >= 4 + kOutWarps) {
+        // lo parts: what a TF32 operand drops of each value, beside the stage, in the same places
+        const int tid = threadIdx.x - (4 + kOutWarps) * 32;
+        constexpr int UNITS = (S::kA + S::kB) / 16;
+        int it = 0;
+        bool live = true;
+        for (int t = first; live && t < tiles; t += step) {
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const int s = it % STAGES;
+                live = mbar_wait(full + 8 * s, (it / STAGES) & 1, abort_flag);
+                live = __all_sync(0xffffffffu, live);
+                if (!live) { report(p.status, 44); break; }
+                const uint32_t raw = ring + s * S::kStage + tid * 16, lo = raw + S::kA + S::kB;
+#pragma unroll 4
+                for (int u = 0; u < UNITS / 128; ++u) {
+                    const float4 v = shared_get(raw + u * 2048);
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(lo + u * 2048), "f"(v.x - tf32_hi(v.x)), "f"(v.y - tf32_hi(v.y)),
+                                 "f"(v.z - tf32_hi(v.z)), "f"(v.w - tf32_hi(v.w))
+                                 : "memory");
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(ready + 8 * s);
+            }
+        }
+    }
+
+    tc_fence_before();
+    if (split > 1) {
+        // every product of the cluster is done, so the rings hold partial tiles only
+        cg::this_cluster().sync();
+        if (warp >= 4 && warp < 4 + kOutWarps && !*abort_flag) {
+            const Tile tile = tile_at(first, p.tiles_m, p.tiles_n);
+            for (int i = warp - 4; i * split + rank < BN / 32 * 4; i += kOutWarps) {
+                const int u = i * split + rank;
+                finish_block<T>(p, ring + u * kBlock, split, tile.m * kTileM + (u & 3) * 32, tile.n * BN + (u >> 2) * 32, lane);
+            }
+        }
+        cg::this_cluster().sync();
+    } else {
+        __syncthreads();
+    }
+    tc_fence_after();
+    if (warp == 2) tmem_dealloc(tmem, 2 * BN);
+}
+
+// ---- dz and its column sums --------------------------------------------------------------------------------------------
+struct DzArgs {
+    const void *dy, *z;
+    void *dz, *db;                   // dz: null where dy itself is read by the products; db may be null
+    int64_t rows, ld, ld_dz;
+    int n, parts, act, db_fp32;
+};
+// A CTA goes down 128 bytes of columns; `parts` CTAs of a cluster share the rows and add their sums up in rank order.
+// WIDE: 16 bytes a thread; else (rows that do not start on 16-byte boundaries) value by value, a row per warp.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ DzArgs p)
+{
+    constexpr int COLS = 128 / sizeof(T);
+    constexpr int V = WIDE ? 16 / (int)sizeof(T) : COLS / 32, STRIDE = WIDE ? 1 : 32, ROWS = WIDE ? 32 : 8;
+    __shared__ float s_sum[8][COLS];
+    __shared__ float s_total[COLS];
+    const int part = (int)(blockIdx.x % (unsigned)p.parts);
+    const int c0 = (int)(blockIdx.x / (unsigned)p.parts) * COLS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col = WIDE ? (threadIdx.x & 7) * V : lane;
+    const int r0 = WIDE ? threadIdx.x >> 3 : warp;
+    float sum[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = 0.f;
+    const bool whole = c0 + col + (V - 1) * STRIDE < p.n;
+#pragma unroll 4
+    for (int64_t r = (int64_t)part * ROWS + r0; r < p.rows; r += (int64_t)p.parts * ROWS) {
+        float g[V], z[V];
+        const T* dy = reinterpret_cast<const T*>(p.dy) + r * p.ld + c0 + col;
+        const T* zr = reinterpret_cast<const T*>(p.z) + r * p.ld + c0 + col;
+        if (WIDE && whole) {
+            if constexpr (WIDE) {
+                Pack<T>::unpack(*reinterpret_cast<const uint4*>(dy), g);
+                if (p.act != HPF_ACT_NONE) Pack<T>::unpack(*reinterpret_cast<const uint4*>(zr), z);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const bool in = c0 + col + j * STRIDE < p.n;
+                g[j] = in ? Pack<T>::get(dy[j * STRIDE]) : 0.f;
+                z[j] = in && p.act != HPF_ACT_NONE ? Pack<T>::get(zr[j * STRIDE]) : 0.f;
+            }
+        }
+        if (p.act != HPF_ACT_NONE) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) g[j] *= slope(z[j], p.act);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += g[j];
+        if (p.dz) {
+            // dz is rounded to the operands' type: the tensor cores take it in that type only
+            T* out = reinterpret_cast<T*>(p.dz) + r * p.ld_dz + c0 + col;
+            if (WIDE && whole) {
+                if constexpr (WIDE) *reinterpret_cast<uint4*>(out) = Pack<T>::pack(g);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (c0 + col + j * STRIDE < p.n) out[j * STRIDE] = Pack<T>::put(g[j]);
+            }
+        }
+    }
+    if (!p.db) return;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (WIDE) {
+            sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 8);
+            sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
+            if (lane < 8) s_sum[warp][col + j] = sum[j];
+        } else {
+            s_sum[warp][col + j * STRIDE] = sum[j];
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < COLS) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t += s_sum[w][threadIdx.x];
+        s_total[threadIdx.x] = t;
+    }
+    if (p.parts > 1) cg::this_cluster().sync();
+    if (part == 0 && threadIdx.x < COLS && c0 + (int)threadIdx.x < p.n) {
+        float t = s_total[threadIdx.x];
+        for (int k = 1; k < p.parts; ++k) t += *cg::this_cluster().map_shared_rank(&s_total[threadIdx.x], k);
+        if (p.db_fp32) reinterpret_cast<float*>(p.db)[c0 + threadIdx.x] = t;
+        else reinterpret_cast<T*>(p.db)[c0 + threadIdx.x] = Pack<T>::put(t);
+    }
+    if (p.parts > 1) cg::this_cluster().sync();
+}
+
+// Rows that a tensor copy cannot address (start or stride off 16 bytes), laid out again at a stride that it can.
+template <typename T>
+__global__ void __launch_bounds__(256) linear_repack_kernel(const T* __restrict__ in, T* __restrict__ out, int64_t rows, int n, int64_t ld, int64_t ld_out)
+{
+    for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (int64_t)gridDim.x * 8)
+        for (int c = threadIdx.x & 31; c < n; c += 32) out[r * ld_out + c] = in[r * ld + c];
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------------------
+size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+int64_t padded(int64_t n, int e) { return (n * e + 15) / 16 * 16 / e; }
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+int sm_count()
+{
+    static PerDevice<int> sms;
+    int n = 0;
+    if (sms.get(&n, [](int dev, int* v) { return cudaDeviceGetAttribute(v, cudaDevAttrMultiProcessorCount, dev); }) != cudaSuccess) return 148;
+    return n;
+}
+
+struct Operand {
+    const void* p;
+    int64_t rows, cols, ld;          // as it lies in memory: cols contiguous
+    bool mn;                         // the contiguous dimension is m / n
+};
+
+template <int E>
+cudaError_t make_map(CUtensorMap* tm, const Operand& o, int32_t dtype, int tile)
+{
+    constexpr int inner = kRow / E;
+    const cuuint64_t dims[2] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)(o.ld * E)};
+    const cuuint32_t box[2] = {(cuuint32_t)inner, (cuuint32_t)(o.mn ? inner : tile)};
+    const cuuint32_t ones[2] = {1, 1};
+    const CUtensorMapDataType type = dtype == HPF_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == HPF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const CUresult r = g_encode(tm, type, 2, const_cast<void*>(o.p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                E == 4 && o.mn ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int E, typename T, int BN, bool PROMOTE>
+cudaError_t launch_gemm(GemmArgs& g, cudaStream_t st)
+{
+    auto* kernel = linear_gemm_kernel<E, T, BN, PROMOTE>;
+    static PerDevice<bool> attributes;
+    bool set = false;
+    cudaError_t e = attributes.get(&set, [&](int, bool* v) { *v = true; return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
+    if (e != cudaSuccess) return e;
+    const int tiles = g.tiles_m * g.tiles_n;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(g.split > 1 ? (unsigned)(tiles * g.split) : (unsigned)(tiles < sm_count() ? tiles : sm_count()));
+    cfg.blockDim = dim3(Shape<E, BN>::kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)g.split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = g.split > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, g);
+}
+
+struct Plan {
+    int bn, split;
+};
+// Tile width and split of k by a modelled time in clocks: waves of CTAs x (stages a CTA runs through x clocks of a stage's MMAs + what
+// a tile costs besides).  Clocks of one MMA (M = 128): 48 at N = 64, 64 at 128, 128 at 256.
+Plan choose(int64_t M, int64_t N, int k_blocks, int widest, int mmas)
+{
+    Plan best{64, 1};
+    double least = 1e300;
+    for (int bn = widest; bn >= 64; bn /= 2) {
+        const int64_t tiles = ((M + kTileM - 1) / kTileM) * ((N + bn - 1) / bn);
+        const double stage = mmas * (bn == 256 ? 128.0 : bn == 128 ? 64.0 : 48.0);
+        for (int split = 1; split <= kMaxSplit; split *= 2) {
+            if (split > 1 && (k_blocks < 2 * split || tiles * split > 2 * sm_count())) break;
+            const int64_t waves = (tiles * split + sm_count() - 1) / sm_count();
+            const double t = waves * (((k_blocks + split - 1) / split) * stage + 6.0 * bn) + 2500.0 + (split > 1 ? 1500.0 : 0.0);
+            if (t < least) { least = t; best = Plan{bn, split}; }
+        }
+    }
+    return best;
+}
+
+// out[M][N] = sum_k A B in the operands' type; out_fp32: the result is fp32 whatever that type is
+template <int E>
+cudaError_t gemm(GemmArgs& g, const Operand& a, const Operand& b, int64_t M, int64_t N, int64_t K, int32_t dtype, bool out_fp32, cudaStream_t st)
+{
+    const bool promote = dtype == HPF_FP32 || out_fp32;
+    const int k_blocks = (int)((K * E + kRow - 1) / kRow);
+    const Plan plan = choose(M, N, k_blocks, promote ? 128 : 256, E == 4 ? 12 : 4);
+    g.M = (int)M; g.N = (int)N; g.k_blocks = k_blocks; g.split = plan.split;
+    g.tiles_m = (int)((M + kTileM - 1) / kTileM);
+    g.tiles_n = (int)((N + plan.bn - 1) / plan.bn);
+    g.a_mn = a.mn; g.b_mn = b.mn;
+    const uint32_t fmt = dtype == HPF_FP32 ? 2u : dtype == HPF_BF16 ? 1u : 0u;
+    g.idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((a.mn ? 1u : 0u) << 15) | ((b.mn ? 1u : 0u) << 16) | ((uint32_t)(plan.bn >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
+    const size_t oe = promote ? 4 : 2;
+    g.wide = aligned16(g.out) && (g.ld * oe) % 16 == 0 && (!g.z || aligned16(g.z)) && (!g.residual || aligned16(g.residual));
+    cudaError_t e = make_map<E>(&g.ta, a, dtype, kTileM);
+    if (e == cudaSuccess) e = make_map<E>(&g.tb, b, dtype, plan.bn);
+    if (e != cudaSuccess) return e;
+    if constexpr (E == 4) {
+        return plan.bn == 128 ? launch_gemm<4, float, 128, true>(g, st) : launch_gemm<4, float, 64, true>(g, st);
+    } else {
+        if (out_fp32) return plan.bn == 128 ? launch_gemm<2, float, 128, true>(g, st) : launch_gemm<2, float, 64, true>(g, st);
+        if (dtype == HPF_BF16)
+            return plan.bn == 256   ? launch_gemm<2, __nv_bfloat16, 256, false>(g, st)
+                   : plan.bn == 128 ? launch_gemm<2, __nv_bfloat16, 128, false>(g, st)
+                                    : launch_gemm<2, __nv_bfloat16, 64, false>(g, st);
+        return plan.bn == 256   ? launch_gemm<2, __half, 256, false>(g, st)
+               : plan.bn == 128 ? launch_gemm<2, __half, 128, false>(g, st)
+                                : launch_gemm<2, __half, 64, false>(g, st);
+    }
+}
+cudaError_t gemm_any(GemmArgs& g, const Operand& a, const Operand& b, int64_t M, int64_t N, int64_t K, int32_t dtype, bool out_fp32, cudaStream_t st)
+{
+    return dtype == HPF_FP32 ? gemm<4>(g, a, b, M, N, K, dtype, out_fp32, st) : gemm<2>(g, a, b, M, N, K, dtype, out_fp32, st);
+}
+
+cudaError_t repack(const void* in, void* out, int64_t rows, int n, int64_t ld, int64_t ld_out, int e, cudaStream_t st)
+{
+    const int64_t blocks = (rows + 7) / 8;
+    const unsigned grid = (unsigned)(blocks < 8 * sm_count() ? blocks : 8 * sm_count());
+    if (e == 4) linear_repack_kernel<uint32_t><<<grid, 256, 0, st>>>(static_cast<const uint32_t*>(in), static_cast<uint32_t*>(out), rows, n, ld, ld_out);
+    else linear_repack_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t*>(in), static_cast<uint16_t*>(out), rows, n, ld, ld_out);
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_dz(DzArgs& a, cudaStream_t st)
+{
+    const int cols = 128 / sizeof(T);
+    const bool wide = aligned16(a.dy) && (a.ld * sizeof(T)) % 16 == 0 && (a.act == HPF_ACT_NONE || aligned16(a.z));
+    const int64_t want = (a.rows + 63) / 64;
+    a.parts = (int)(want < 1 ? 1 : want > 8 ? 8 : want);
+    auto* kernel = wide ? linear_dz_kernel<T, true> : linear_dz_kernel<T, false>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((a.n + cols - 1) / cols * a.parts));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)a.parts;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.parts > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+// ---- scratch: status word | dz | x laid out again | W laid out again ----------------------------------------------------
+struct Scratch {
+    size_t dz, x, w, total;
+};
+// x_ok, w_ok, dy_ok: a tensor copy can address the rows as they lie
+Scratch scratch_of(int64_t rows, int n_in, int n_out, int e, bool x_ok, bool w_ok, bool dy_ok, int act, bool bwd)
+{
+    Scratch s;
+    s.dz = 256;
+    s.x = s.dz + (bwd && (act != HPF_ACT_NONE || !dy_ok) ? up((size_t)rows * padded(n_out, e) * e, 256) : 0);
+    s.w = s.x + (x_ok ? 0 : up((size_t)rows * padded(n_in, e) * e, 256));
+    s.total = s.w + (w_ok ? 0 : up((size_t)n_out * padded(n_in, e) * e, 256));
+    return s;
+}
+int check(int64_t rows, int32_t n_in, int32_t n_out, int64_t ld_x, int64_t ld_y, int32_t dtype, int32_t act)
+{
+    if (dtype != HPF_FP32 && dtype != HPF_BF16 && dtype != HPF_FP16) return api_fail(HPF_ERR_INVALID, "dtype must be HPF_FP32, HPF_BF16 or HPF_FP16");
+    if (act < HPF_ACT_NONE || act > HPF_ACT_SILU) return api_fail(HPF_ERR_INVALID, "unknown activation");
+    if (rows < 0 || n_in < 1 || n_out < 1 || ld_x < n_in || ld_y < n_out) return api_fail(HPF_ERR_INVALID, "rows < 0, an empty side, or a row stride below the row's length");
+    if (rows > (1 << 30) || n_in > (1 << 30) || n_out > (1 << 30)) return api_fail(HPF_ERR_UNSUPPORTED, "more than 2^30 rows, inputs or outputs");
+    // a tensor copy's strides end at 2^40 bytes, a launch at 2^31 tiles
+    if (ld_x > (1ll << 36) || ld_y > (1ll << 36)) return api_fail(HPF_ERR_UNSUPPORTED, "a row stride above 2^36");
+    const int64_t tm = (rows + kTileM - 1) / kTileM, ti = (n_in + 63) / 64, to = (n_out + 63) / 64;
+    if (tm * ti > 0x3fffffff || tm * to > 0x3fffffff || (to + 1) * ti > 0x3fffffff) return api_fail(HPF_ERR_UNSUPPORTED, "more than 2^30 tiles");
+    return HPF_OK;
+}
+bool value_aligned(const void* p, int e) { return (reinterpret_cast<uintptr_t>(p) & (e - 1)) == 0; }
+bool row_ok(const void* p, int64_t ld, int e) { return aligned16(p) && (ld * e) % 16 == 0; }
+
+}  // namespace
+}  // namespace hpf
+
+using namespace hpf;
+
+extern "C" int hpf_linear_scratch_bytes(int64_t rows, int32_t n_in, int32_t n_out, int64_t ld_x, int64_t ld_y, int32_t dtype, int32_t act, int32_t aligned, size_t* bytes)
+{
+    if (!bytes) return api_fail(HPF_ERR_INVALID, "null argument");
+    const int bad = check(rows, n_in, n_out, ld_x, ld_y, dtype, act);
+    if (bad != HPF_OK) return bad;
+    const int e = dtype == HPF_FP32 ? 4 : 2;
+    *bytes = scratch_of(rows, n_in, n_out, e, aligned && (ld_x * e) % 16 == 0, aligned && ((int64_t)n_in * e) % 16 == 0, aligned && (ld_y * e) % 16 == 0, act, true).total;
+    return HPF_OK;
+}
+
+extern "C" int hpf_linear_fwd(const void* d_x, const void* d_w, const void* d_bias, const void* d_residual, void* d_y, void* d_z, int64_t rows,
+                              int32_t n_in, int32_t n_out, int64_t ld_x, int64_t ld_y, int32_t dtype, int32_t act, void* d_scratch,
+                              size_t scratch_bytes, void* stream)
+{
+    const int bad = check(rows, n_in, n_out, ld_x, ld_y, dtype, act);
+    if (bad != HPF_OK) return bad;
+    if (rows == 0) return HPF_OK;
+    const int e = dtype == HPF_FP32 ? 4 : 2;
+    if (!d_x || !d_w || !d_y || !d_scratch) return api_fail(HPF_ERR_INVALID, "null argument");
+    for (const void* p : {d_x, d_w, d_bias, d_residual, static_cast<const void*>(d_y), static_cast<const void*>(d_z)})
+        if (!value_aligned(p, e)) return api_fail(HPF_ERR_INVALID, "a tensor is not aligned to its type");
+    const bool x_ok = row_ok(d_x, ld_x, e), w_ok = row_ok(d_w, n_in, e);
+    const Scratch s = scratch_of(rows, n_in, n_out, e, x_ok, w_ok, true, act, false);
+    if (!aligned16(d_scratch) || scratch_bytes < s.total) return api_fail(HPF_ERR_WORKSPACE, "scratch too small or misaligned (hpf_linear_scratch_bytes)");
+    cudaError_t ce = conv_tc_init();
+    if (ce != cudaSuccess) return api_cuda_fail(ce, "hpf_linear_fwd: set-up");
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    char* base = static_cast<char*>(d_scratch);
+    Operand x{d_x, rows, n_in, ld_x, false}, w{d_w, n_out, n_in, n_in, false};
+    if (!x_ok) { ce = repack(d_x, base + s.x, rows, n_in, ld_x, padded(n_in, e), e, st); x.p = base + s.x; x.ld = padded(n_in, e); }
+    if (ce == cudaSuccess && !w_ok) { ce = repack(d_w, base + s.w, n_out, n_in, n_in, padded(n_in, e), e, st); w.p = base + s.w; w.ld = padded(n_in, e); }
+    if (ce != cudaSuccess) return api_cuda_fail(ce, "hpf_linear_fwd: layout");
+    GemmArgs g = {};
+    g.act = act; g.out = d_y; g.z = d_z; g.bias = d_bias; g.residual = d_residual; g.ld = ld_y;
+    g.status = reinterpret_cast<DeviceStatus*>(d_scratch);
+    ce = gemm_any(g, x, w, rows, n_out, n_in, dtype, false, st);
+    return ce == cudaSuccess ? HPF_OK : api_cuda_fail(ce, "hpf_linear_fwd");
+}
+
+extern "C" int hpf_linear_bwd(const void* d_dy, const void* d_z, const void* d_x, const void* d_w, void* d_dx, void* d_dw, void* d_dbias, int64_t rows,
+                              int32_t n_in, int32_t n_out, int64_t ld_x, int64_t ld_y, int32_t dtype, int32_t act, int32_t grad_type,
+                              void* d_scratch, size_t scratch_bytes, void* stream)
+{
+    const int bad = check(rows, n_in, n_out, ld_x, ld_y, dtype, act);
+    if (bad != HPF_OK) return bad;
+    if (grad_type != dtype && grad_type != HPF_FP32) return api_fail(HPF_ERR_INVALID, "grad_type must be dtype or HPF_FP32");
+    const int e = dtype == HPF_FP32 ? 4 : 2, ge = grad_type == HPF_FP32 ? 4 : 2;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (!value_aligned(d_dw, ge) || !value_aligned(d_dbias, ge)) return api_fail(HPF_ERR_INVALID, "a tensor is not aligned to its type");
+    if (rows == 0) {
+        // an empty batch: sums of nothing
+        cudaError_t ce = d_dw ? cudaMemsetAsync(d_dw, 0, (size_t)n_out * n_in * ge, st) : cudaSuccess;
+        if (ce == cudaSuccess && d_dbias) ce = cudaMemsetAsync(d_dbias, 0, (size_t)n_out * ge, st);
+        return ce == cudaSuccess ? HPF_OK : api_cuda_fail(ce, "hpf_linear_bwd: empty batch");
+    }
+    if (!d_dy || (d_dx && !d_w) || (d_dw && !d_x) || (act != HPF_ACT_NONE && !d_z) || !d_scratch) return api_fail(HPF_ERR_INVALID, "null argument");
+    for (const void* p : {d_dy, d_z, d_x, d_w, static_cast<const void*>(d_dx)})
+        if (!value_aligned(p, e)) return api_fail(HPF_ERR_INVALID, "a tensor is not aligned to its type");
+    const bool x_ok = !d_dw || row_ok(d_x, ld_x, e), w_ok = !d_dx || row_ok(d_w, n_in, e), dy_ok = row_ok(d_dy, ld_y, e);
+    const bool products = d_dx || d_dw;
+    const Scratch s = scratch_of(rows, n_in, n_out, e, x_ok, w_ok, dy_ok || !products, products ? act : HPF_ACT_NONE, true);
+    if (!aligned16(d_scratch) || scratch_bytes < s.total) return api_fail(HPF_ERR_WORKSPACE, "scratch too small or misaligned (hpf_linear_scratch_bytes)");
+    cudaError_t ce = conv_tc_init();
+    if (ce != cudaSuccess) return api_cuda_fail(ce, "hpf_linear_bwd: set-up");
+    char* base = static_cast<char*>(d_scratch);
+    DzArgs d = {};
+    const bool own_dz = products && (act != HPF_ACT_NONE || !dy_ok);
+    d.dy = d_dy; d.z = d_z; d.dz = own_dz ? base + s.dz : nullptr; d.db = d_dbias;
+    d.rows = rows; d.ld = ld_y; d.ld_dz = padded(n_out, e); d.n = n_out; d.act = act; d.db_fp32 = grad_type == HPF_FP32;
+    if (own_dz || d_dbias) {
+        ce = dtype == HPF_FP32 ? launch_dz<float>(d, st) : dtype == HPF_BF16 ? launch_dz<__nv_bfloat16>(d, st) : launch_dz<__half>(d, st);
+        if (ce != cudaSuccess) return api_cuda_fail(ce, "hpf_linear_bwd: dz");
+    }
+    const void* dz = own_dz ? base + s.dz : d_dy;
+    const int64_t ld_dz = own_dz ? d.ld_dz : ld_y;
+    GemmArgs g = {};
+    g.status = reinterpret_cast<DeviceStatus*>(d_scratch);
+    if (d_dx) {
+        Operand a{dz, rows, n_out, ld_dz, false}, w{d_w, n_out, n_in, n_in, true};
+        if (!w_ok) { ce = repack(d_w, base + s.w, n_out, n_in, n_in, padded(n_in, e), e, st); w.p = base + s.w; w.ld = padded(n_in, e); }
+        g.out = d_dx; g.ld = ld_x;
+        if (ce == cudaSuccess) ce = gemm_any(g, a, w, rows, n_in, n_out, dtype, false, st);
+        if (ce != cudaSuccess) return api_cuda_fail(ce, "hpf_linear_bwd: dx");
+    }
+    if (d_dw) {
+        Operand a{dz, rows, n_out, ld_dz, true}, x{d_x, rows, n_in, ld_x, true};
+        if (!x_ok) { ce = repack(d_x, base + s.x, rows, n_in, ld_x, padded(n_in, e), e, st); x.p = base + s.x; x.ld = padded(n_in, e); }
+        g.out = d_dw; g.ld = n_in;
+        if (ce == cudaSuccess) ce = gemm_any(g, a, x, n_out, n_in, rows, dtype, grad_type == HPF_FP32, st);
+        if (ce != cudaSuccess) return api_cuda_fail(ce, "hpf_linear_bwd: dW");
+    }
+    return HPF_OK;
+}
+
+extern "C" int hpf_linear_status(const void* d_scratch, int32_t* h_gave_up)
+{
+    if (!d_scratch || !h_gave_up) return api_fail(HPF_ERR_INVALID, "null argument");
+    DeviceStatus s = {};
+    const cudaError_t e = cudaMemcpy(&s, d_scratch, sizeof(s), cudaMemcpyDeviceToHost);
+    if (e != cudaSuccess) return api_cuda_fail(e, "hpf_linear_status");
+    *h_gave_up = s.code != 0;
+    return HPF_OK;
+}
