@@ -12,7 +12,7 @@
 // warps write lo beside each stage and three MMAs form hi hi + lo hi + hi lo.  What is left out of a product (lo lo, and the bits of a lo
 // that TF32 drops) is below 3 2^-20 of it, about 2^-21 on average.
 // The accumulator truncates each addition, an error that grows with the number of additions and always points to zero: where the
-// result is fp32, sums are taken out of TMEM every kChunk stages and added up in registers, rounded to nearest.
+// result is fp32, sums are taken out of TMEM every few stages and added up in registers, rounded to nearest.
 //
 // Few tiles (few rows, small layers): the k loop is split over a cluster of up to 8 CTAs.  Each leaves its fp32 partial tile in
 // its own shared memory; the CTAs then add the partial tiles up over distributed shared memory, always in rank order.
@@ -37,13 +37,16 @@ constexpr int kRing = 192 * 1024;              // bytes of the ring of stages
 constexpr int kBlock = 4096;                   // a 32 x 32 block of fp32 on its way out
 constexpr int kOutWarps = 8;
 constexpr int kSmem = kRing + kOutWarps * kBlock + 1024 + 512;
-constexpr int kChunk = 4;                      // stages whose products are added up in TMEM where the result is fp32
+constexpr int kMaxStages = 8;
 constexpr int kMaxSplit = 8;
 
 struct GemmArgs {
     CUtensorMap ta, tb;
-    int M, N, k_blocks, tiles_m, tiles_n, split;
+    int rows, cols;                            // of out
+    int k_blocks, tiles_m, tiles_n, split;
+    int swap;                                  // few rows: a tile's 128 lanes are columns of out, its BN columns rows of out
     int a_mn, b_mn;                            // operand has m / n contiguous (else k)
+    int a_box, b_box;                          // rows of m / n that a k-contiguous stage is filled with (the rest is never looked at)
     uint32_t idesc;
     int act, wide;                             // wide: every output and the residual take 16-byte accesses
     void *out, *z;
@@ -140,23 +143,70 @@ template <> struct Pack<__half> {
     static __device__ __forceinline__ __half put(float v) { return __float2half_rn(v); }
 };
 
-// gelu is z Phi(z) with the error function, silu z / (1 + e^-z)
-__device__ __forceinline__ float activate(float z, int act)
+__device__ __forceinline__ float ex2(float x)
 {
-    if (act == HPF_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
-    if (act == HPF_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678f));
-    if (act == HPF_ACT_SILU) return z / (1.f + expf(-z));
-    return z;
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-__device__ __forceinline__ float slope(float z, int act)
+__device__ __forceinline__ float reciprocal(float x)
 {
-    if (act == HPF_ACT_RELU) return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    if (act == HPF_ACT_GELU) return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
-    if (act == HPF_ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-z));
-        return s * fmaf(z, 1.f - s, 1.f);
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// gelu is z Phi(z), its slope Phi(z) + z phi(z).  Phi by Abramowitz and Stegun 7.1.26: with x = |z| / sqrt 2 and t = 1 / (1 + p x),
+// 1 - erf x = (a1 t + ... + a5 t^5) e^(-x^2) within 1.5e-7, and e^(-x^2) = e^(-z^2 / 2) is what phi needs too: 2 special-function
+// results a value where erff and expf took about 60 instructions (the dz kernel of 8192 x 16384 bf16: 354 us with those).
+__device__ __forceinline__ void gauss(float z, float* cdf, float* bell)
+{
+    const float x = fabsf(z) * 0.70710678118f;
+    const float t = reciprocal(fmaf(0.3275911f, x, 1.f));
+    const float e = ex2(z * z * -0.72134752044f);
+    const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    *cdf = z > 0.f ? 1.f - tail : tail;
+    *bell = e * 0.39894228040f;
+}
+__device__ __forceinline__ float sigmoid(float z) { return reciprocal(1.f + ex2(z * -1.44269504089f)); }
+template <int V>
+__device__ __forceinline__ void activate(float* v, int act)
+{
+    if (act == HPF_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = v[j] < 0.f ? 0.f : v[j];          // a NaN stays
+    } else if (act == HPF_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float cdf, bell;
+            gauss(v[j], &cdf, &bell);
+            v[j] *= cdf;
+        }
+    } else if (act == HPF_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] *= sigmoid(v[j]);
     }
-    return 1.f;
+}
+// g *= act'(z)
+template <int V>
+__device__ __forceinline__ void apply_slope(float* g, const float* z, int act)
+{
+    if (act == HPF_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) g[j] = z[j] > 0.f ? g[j] : z[j] != z[j] ? z[j] : 0.f;
+    } else if (act == HPF_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float cdf, bell;
+            gauss(z[j], &cdf, &bell);
+            g[j] *= fmaf(z[j], bell, cdf);
+        }
+    } else if (act == HPF_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float s = sigmoid(z[j]);
+            g[j] *= s * fmaf(z[j], 1.f - s, 1.f);
+        }
+    }
 }
 
 // ---- the product ------------------------------------------------------------------------------------------------------
@@ -174,97 +224,150 @@ __device__ __forceinline__ Tile tile_at(int t, int tiles_m, int tiles_n)
 // Where 16-byte unit u of row r of a 32 x 32 block lies: units of a row are spread so that both the writers (a row per lane) and the
 // readers (a few rows at a time) touch all banks.
 __device__ __forceinline__ uint32_t unit_at(uint32_t block, int r, int u) { return block + r * 128 + ((u ^ (r & 7)) << 4); }
-__device__ __forceinline__ void block_put(uint32_t block, int lane, const float* v)
+// A lane's 32 values as row `lane` of the block, or (swapped) as column `lane`.
+__device__ __forceinline__ void block_put(uint32_t block, int lane, const float* v, int swap)
 {
+    if (!swap) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(unit_at(block, lane, u)), "f"(v[4 * u]), "f"(v[4 * u + 1]), "f"(v[4 * u + 2]), "f"(v[4 * u + 3])
-                     : "memory");
+        for (int u = 0; u < 8; ++u)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(unit_at(block, lane, u)), "f"(v[4 * u]), "f"(v[4 * u + 1]), "f"(v[4 * u + 2]), "f"(v[4 * u + 3])
+                         : "memory");
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(unit_at(block, j, lane >> 2) + (lane & 3) * 4), "f"(v[j]) : "memory");
+    }
 }
-__device__ __forceinline__ float4 shared_get(uint32_t addr)
+__device__ __forceinline__ float4 shared_get4(uint32_t addr)
 {
     float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
     return v;
 }
-__device__ __forceinline__ float4 cluster_get(uint32_t addr, int rank)
+__device__ __forceinline__ float shared_get(uint32_t addr)
 {
-    float4 v;
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank)
+{
     uint32_t there;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+    return there;
+}
+__device__ __forceinline__ float4 cluster_get4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
     return v;
+}
+// the sum of the cluster's values at one place, in rank order; all loads are under way before the first is needed
+__device__ __forceinline__ float4 cluster_sum4(uint32_t addr, int split)
+{
+    float4 part[kMaxSplit];
+#pragma unroll
+    for (int k = 0; k < kMaxSplit; ++k)
+        if (k < split) part[k] = cluster_get4(at_rank(addr, k));
+    float4 s = part[0];
+#pragma unroll
+    for (int k = 1; k < kMaxSplit; ++k)
+        if (k < split) { s.x += part[k].x; s.y += part[k].y; s.z += part[k].z; s.w += part[k].w; }
+    return s;
 }
 
-// One warp finishes the 32 x 32 block whose fp32 sums lie in shared memory (of `split` CTAs, added up in rank order): bias,
-// activation, residual, one rounding.  A lane holds 16 bytes of a row, so every access to memory is whole sectors.
+// The last steps on V values of one row of out that start at column col: bias, activation, residual, one rounding.
 template <typename T>
-__device__ __forceinline__ void finish_block(const GemmArgs& p, uint32_t block, int split, int row0, int col0, int lane)
+__device__ __forceinline__ void finish_wide(const GemmArgs& p, float* v, const float* bias, int row, int col)
+{
+    constexpr int V = Pack<T>::V;
+    const int64_t at = row * p.ld + col;
+    uint4 res;
+    if (p.residual) res = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.residual) + at);
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] += bias[j];
+    if (p.z) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.z) + at) = Pack<T>::pack(v);
+    if (p.act != HPF_ACT_NONE) activate<V>(v, p.act);
+    if (p.residual) {
+        float f[V];
+        Pack<T>::unpack(res, f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] += f[j];
+    }
+    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + at) = Pack<T>::pack(v);
+}
+template <typename T>
+__device__ __forceinline__ void finish_one(const GemmArgs& p, float v, float bias, int row, int col)
+{
+    const int64_t at = row * p.ld + col;
+    v += bias;
+    if (p.z) reinterpret_cast<T*>(p.z)[at] = Pack<T>::put(v);
+    if (p.act != HPF_ACT_NONE) activate<1>(&v, p.act);
+    if (p.residual) v += Pack<T>::get(reinterpret_cast<const T*>(p.residual)[at]);
+    reinterpret_cast<T*>(p.out)[at] = Pack<T>::put(v);
+}
+// One warp finishes rows [from, to) of the 32 x 32 block of out at (row0, col0) whose fp32 sums lie in shared memory (SPLIT: of all CTAs
+// of the cluster).  16 bytes of a row per lane where rows lie on 16-byte boundaries, else a column per lane: either way an access is
+// whole sectors.  The loops stay rolled: unrolled, this code no longer fitted the instruction
+// caches and a 128 x 128 tile took 4 us to write out.
+template <typename T, bool SPLIT>
+__device__ __forceinline__ void finish_block(const GemmArgs& p, uint32_t block, int row0, int col0, int from, int to, int lane)
 {
     constexpr int V = Pack<T>::V, PER_ROW = 32 / V, ROWS = 32 / PER_ROW;
-    const int col = col0 + (lane % PER_ROW) * V;
-    if (row0 >= p.M || col >= p.N) return;
-    const bool wide = p.wide && col + V <= p.N;
-    float bias[V];
+    const int rows = min(to, p.rows - row0);
+    if (rows <= from || col0 >= p.cols) return;
+    if (p.wide && col0 + 32 <= p.cols) {
+        const int c = (lane % PER_ROW) * V, col = col0 + c;
+        float bias[V];
+        if (p.bias) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) bias[j] = p.bias && col + j < p.N ? Pack<T>::get(reinterpret_cast<const T*>(p.bias)[col + j]) : 0.f;
+            for (int j = 0; j < V; ++j) bias[j] = Pack<T>::get(reinterpret_cast<const T*>(p.bias)[col + j]);
+        } else {
 #pragma unroll
-    for (int i = 0; i < PER_ROW; ++i) {
-        const int r = i * ROWS + lane / PER_ROW, row = row0 + r;
-        if (row >= p.M) continue;
-        float v[V];
+            for (int j = 0; j < V; ++j) bias[j] = 0.f;
+        }
+#pragma unroll 1
+        for (int r = from + lane / PER_ROW; r < rows; r += ROWS) {
+            float v[V];
 #pragma unroll
-        for (int h = 0; h < V / 4; ++h) {
-            const uint32_t at = unit_at(block, r, (lane % PER_ROW) * (V / 4) + h);
-            float4 s = split == 1 ? shared_get(at) : cluster_get(at, 0);
-            for (int k = 1; k < split; ++k) {
-                const float4 o = cluster_get(at, k);
-                s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+            for (int h = 0; h < V / 4; ++h) {
+                const uint32_t at = unit_at(block, r, (lane % PER_ROW) * (V / 4) + h);
+                const float4 s = SPLIT ? cluster_sum4(at, p.split) : shared_get4(at);
+                v[4 * h] = s.x; v[4 * h + 1] = s.y; v[4 * h + 2] = s.z; v[4 * h + 3] = s.w;
             }
-            v[4 * h] = s.x; v[4 * h + 1] = s.y; v[4 * h + 2] = s.z; v[4 * h + 3] = s.w;
+            finish_wide<T>(p, v, bias, row0 + r, col);
         }
-        const int64_t at = row * p.ld + col;
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] += bias[j];
-        if (p.z) {
-            T* z = reinterpret_cast<T*>(p.z) + at;
-            if (wide) *reinterpret_cast<uint4*>(z) = Pack<T>::pack(v);
-            else
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (col + j < p.N) z[j] = Pack<T>::put(v[j]);
+    } else if (col0 + lane < p.cols) {
+        const int col = col0 + lane;
+        const float bias = p.bias ? Pack<T>::get(reinterpret_cast<const T*>(p.bias)[col]) : 0.f;
+#pragma unroll 1
+        for (int r = from; r < rows; ++r) {
+            const uint32_t at = unit_at(block, r, lane >> 2) + (lane & 3) * 4;
+            float v = 0.f;
+            if (SPLIT) {
+                for (int k = 0; k < p.split; ++k) {
+                    float o;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o) : "r"(at_rank(at, k)));
+                    v += o;
+                }
+            } else {
+                v = shared_get(at);
+            }
+            finish_one<T>(p, v, bias, row0 + r, col);
         }
-        if (p.act != HPF_ACT_NONE) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = activate(v[j], p.act);
-        }
-        if (p.residual) {
-            const T* res = reinterpret_cast<const T*>(p.residual) + at;
-            float f[V];
-            if (wide) Pack<T>::unpack(*reinterpret_cast<const uint4*>(res), f);
-            else
-#pragma unroll
-                for (int j = 0; j < V; ++j) f[j] = col + j < p.N ? Pack<T>::get(res[j]) : 0.f;
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[j] += f[j];
-        }
-        T* out = reinterpret_cast<T*>(p.out) + at;
-        if (wide) *reinterpret_cast<uint4*>(out) = Pack<T>::pack(v);
-        else
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (col + j < p.N) out[j] = Pack<T>::put(v[j]);
     }
 }
 
-// E: bytes of an operand value (2: fp16 / bf16, 4: fp32 as three TF32 products).  PROMOTE: sums leave TMEM every kChunk stages.
+// E: bytes of an operand value (2: fp16 / bf16, 4: fp32 as three TF32 products).  PROMOTE: sums leave TMEM every few stages.
 template <int E, int BN>
 struct Shape {
     static constexpr int kA = kTileM * kRow, kB = BN * kRow;
     static constexpr int kStage = (kA + kB) * (E == 4 ? 2 : 1);
-    static constexpr int kStages = kRing / kStage;
+    static constexpr int kStages = kRing / kStage < kMaxStages ? kRing / kStage : kMaxStages;
     static constexpr int kThreads = (4 + kOutWarps + (E == 4 ? 4 : 0)) * 32;
     static constexpr int kInner = kRow / E;              // values in a row of a stage
+    // Stages whose products are added up in TMEM where the result is fp32: 12 or 16 truncating additions.  (fp32 operands: with 4
+    // stages, 48 additions, a product of K = 2048 was 1.2e-6 off, with 1 stage it is as far off as one summed in fp32 FMAs.)
+    static constexpr int kChunk = E == 4 ? 1 : 4;
 };
 
 template <int E, typename T, int BN, bool PROMOTE>
@@ -273,12 +376,12 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
     using S = Shape<E, BN>;
     constexpr int STAGES = S::kStages;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) unsigned long long s_bars[3 * 8 + 4];
+    __shared__ __align__(8) unsigned long long s_bars[3 * kMaxStages + 4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t staging = ring + kRing;
-    const uint32_t full = smem_u32(s_bars), empty = full + 64, ready = full + 128, acc_full = full + 192, acc_empty = acc_full + 16;
+    const uint32_t full = smem_u32(s_bars), empty = full + 8 * kMaxStages, ready = empty + 8 * kMaxStages, acc_full = ready + 8 * kMaxStages, acc_empty = acc_full + 16;
     const int warp = warp_index(), lane = threadIdx.x & 31;
     const int split = p.split;
     const int rank = split > 1 ? (int)(blockIdx.x % (unsigned)split) : 0;
@@ -310,6 +413,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
         if (elect_one()) {
             prefetch_tmap(&p.ta);
             prefetch_tmap(&p.tb);
+            const uint32_t bytes = (p.a_mn ? S::kA : p.a_box * kRow) + (p.b_mn ? S::kB : p.b_box * kRow);
             int it = 0;
             bool live = true;
             for (int t = first; live && t < tiles; t += step) {
@@ -318,7 +422,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                     const int s = it % STAGES;
                     if (!mbar_wait(empty + 8 * s, ((it / STAGES) & 1) ^ 1, abort_flag)) { report(p.status, 40); live = false; break; }
                     const uint32_t a = ring + s * S::kStage, b = a + S::kA, bar = full + 8 * s;
-                    mbar_expect_tx(bar, S::kA + S::kB);
+                    mbar_expect_tx(bar, bytes);
                     const int k = kb * S::kInner;
                     if (p.a_mn) {
 #pragma unroll
@@ -326,7 +430,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                     } else {
                         tma_load_2d(a, &p.ta, bar, k, tile.m * kTileM);
                     }
-                    if (p.b_mn) {
+                    if (p.b_mn) {                              // (never with BN = 32: few rows are k-contiguous)
 #pragma unroll
                         for (int i = 0; i < BN / S::kInner; ++i) tma_load_2d(b + i * S::kInner * kRow, &p.tb, bar, tile.n * BN + i * S::kInner, k);
                     } else {
@@ -346,7 +450,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
             bool live = true;
             for (int t = first; live && t < tiles; t += step) {
                 for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int in_chunk = PROMOTE ? (kb - kb0) % kChunk : kb - kb0;
+                    const int in_chunk = PROMOTE ? (kb - kb0) % S::kChunk : kb - kb0;
                     const int buf = chunk & 1;
                     if (in_chunk == 0) {
                         if (!mbar_wait(acc_empty + 8 * buf, ((chunk >> 1) & 1) ^ 1, abort_flag)) { report(p.status, 41); live = false; break; }
@@ -379,7 +483,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                         }
                     }
                     umma_commit(empty + 8 * s);
-                    if (kb + 1 == kb1 || (PROMOTE && in_chunk + 1 == kChunk)) {
+                    if (kb + 1 == kb1 || (PROMOTE && in_chunk + 1 == S::kChunk)) {
                         umma_commit(acc_full + 8 * buf);
                         ++chunk;
                     }
@@ -391,50 +495,54 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
         __syncwarp();
     } else if (warp >= 4 && warp < 4 + kOutWarps) {
         const int quad = warp & 3, half = (warp - 4) >> 2;
-        constexpr int BLOCKS = BN / 64;                       // blocks of 32 columns of this warp
+        constexpr int BLOCKS = BN / 64 > 0 ? BN / 64 : 1;     // blocks of 32 columns of this warp (BN = 32: of the first four warps)
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t mine = staging + (warp - 4) * kBlock;
         int chunk = 0;
         bool live = true;
         for (int t = first; live && t < tiles; t += step) {
             const Tile tile = tile_at(t, p.tiles_m, p.tiles_n);
-            const int row0 = tile.m * kTileM + quad * 32;
+            // block c of the tile, once its sums are in the warp's registers
+            const auto hand_over = [&](int c, const float* v) {
+                if (split > 1) {
+                    block_put(ring + (c * 4 + quad) * kBlock, lane, v, p.swap);
+                } else {
+                    block_put(mine, lane, v, p.swap);
+                    __syncwarp();
+                    const int at_m = tile.m * kTileM + quad * 32, at_n = tile.n * BN + c * 32;
+                    finish_block<T, false>(p, mine, p.swap ? at_n : at_m, p.swap ? at_m : at_n, 0, 32, lane);
+                    __syncwarp();
+                }
+            };
             if constexpr (PROMOTE) {
                 float acc[BLOCKS][32];
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) acc[b][j] = 0.f;
-                for (int kb = kb0; live && kb < kb1; kb += kChunk, ++chunk) {
+                for (int kb = kb0; live && kb < kb1; kb += S::kChunk, ++chunk) {
                     const int buf = chunk & 1;
                     live = mbar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, abort_flag);
                     live = __all_sync(0xffffffffu, live);
                     if (!live) { report(p.status, 43); break; }
                     tc_fence_after();
+                    if (BN > 32 || half == 0) {
 #pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b) {
-                        float v[32];
-                        const uint32_t at = tmem + lanes + buf * BN + (half * BLOCKS + b) * 32;
-                        tmem_ld32(at, v);
+                        for (int b = 0; b < BLOCKS; ++b) {
+                            float v[32];
+                            tmem_ld32(tmem + lanes + buf * BN + (half * BLOCKS + b) * 32, v);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) acc[b][j] += v[j];
+                            for (int j = 0; j < 32; ++j) acc[b][j] += v[j];
+                        }
                     }
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
                 }
                 if (!live) break;
+                if (BN > 32 || half == 0) {
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) {
-                    const int c = half * BLOCKS + b;
-                    if (split > 1) {
-                        block_put(ring + (c * 4 + quad) * kBlock, lane, acc[b]);
-                    } else {
-                        block_put(mine, lane, acc[b]);
-                        __syncwarp();
-                        finish_block<T>(p, mine, 1, row0, tile.n * BN + c * 32, lane);
-                        __syncwarp();
-                    }
+                    for (int b = 0; b < BLOCKS; ++b) hand_over(half * BLOCKS + b, acc[b]);
                 }
             } else {
                 const int buf = chunk & 1;
@@ -447,21 +555,13 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                 for (int b = 0; b < BLOCKS; ++b) {
                     const int c = half * BLOCKS + b;
                     float v[32];
-                    const uint32_t at = tmem + lanes + buf * BN + c * 32;
-                    tmem_ld32(at, v);
+                    if (BN > 32 || half == 0) tmem_ld32(tmem + lanes + buf * BN + c * 32, v);
                     if (b == BLOCKS - 1) {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
                     }
-                    if (split > 1) {
-                        block_put(ring + (c * 4 + quad) * kBlock, lane, v);
-                    } else {
-                        block_put(mine, lane, v);
-                        __syncwarp();
-                        finish_block<T>(p, mine, 1, row0, tile.n * BN + c * 32, lane);
-                        __syncwarp();
-                    }
+                    if (BN > 32 || half == 0) hand_over(c, v);
                 }
             }
         }
@@ -478,12 +578,18 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                 live = __all_sync(0xffffffffu, live);
                 if (!live) { report(p.status, 44); break; }
                 const uint32_t raw = ring + s * S::kStage + tid * 16, lo = raw + S::kA + S::kB;
-#pragma unroll 4
-                for (int u = 0; u < UNITS / 128; ++u) {
-                    const float4 v = shared_get(raw + u * 2048);
-                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(lo + u * 2048), "f"(v.x - tf32_hi(v.x)), "f"(v.y - tf32_hi(v.y)),
-                                 "f"(v.z - tf32_hi(v.z)), "f"(v.w - tf32_hi(v.w))
-                                 : "memory");
+#pragma unroll
+                for (int u = 0; u < UNITS / 128; u += 4) {
+                    float4 v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (u + i < UNITS / 128) v[i] = shared_get4(raw + (u + i) * 2048);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (u + i < UNITS / 128)
+                            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(lo + (u + i) * 2048), "f"(v[i].x - tf32_hi(v[i].x)), "f"(v[i].y - tf32_hi(v[i].y)),
+                                     "f"(v[i].z - tf32_hi(v[i].z)), "f"(v[i].w - tf32_hi(v[i].w))
+                                     : "memory");
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -498,9 +604,10 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
         cg::this_cluster().sync();
         if (warp >= 4 && warp < 4 + kOutWarps && !*abort_flag) {
             const Tile tile = tile_at(first, p.tiles_m, p.tiles_n);
-            for (int i = warp - 4; i * split + rank < BN / 32 * 4; i += kOutWarps) {
-                const int u = i * split + rank;
-                finish_block<T>(p, ring + u * kBlock, split, tile.m * kTileM + (u & 3) * 32, tile.n * BN + (u >> 2) * 32, lane);
+            // quarters of blocks, 8 rows each, dealt out to the ranks and their warps
+            for (int i = (warp - 4) * split + rank; i < BN / 32 * 16; i += kOutWarps * split) {
+                const int u = i >> 2, from = (i & 3) * 8, at_m = tile.m * kTileM + (u & 3) * 32, at_n = tile.n * BN + (u >> 2) * 32;
+                finish_block<T, true>(p, ring + u * kBlock, p.swap ? at_n : at_m, p.swap ? at_m : at_n, from, from + 8, lane);
             }
         }
         cg::this_cluster().sync();
@@ -554,10 +661,7 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ 
                 z[j] = in && p.act != HPF_ACT_NONE ? Pack<T>::get(zr[j * STRIDE]) : 0.f;
             }
         }
-        if (p.act != HPF_ACT_NONE) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) g[j] *= slope(z[j], p.act);
-        }
+        if (p.act != HPF_ACT_NONE) apply_slope<V>(g, z, p.act);
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[j] += g[j];
         if (p.dz) {
@@ -627,13 +731,14 @@ struct Operand {
     bool mn;                         // the contiguous dimension is m / n
 };
 
+// box: rows of m / n of a k-contiguous stage
 template <int E>
-cudaError_t make_map(CUtensorMap* tm, const Operand& o, int32_t dtype, int tile)
+cudaError_t make_map(CUtensorMap* tm, const Operand& o, int32_t dtype, int box_rows)
 {
     constexpr int inner = kRow / E;
     const cuuint64_t dims[2] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows};
     const cuuint64_t strides[1] = {(cuuint64_t)(o.ld * E)};
-    const cuuint32_t box[2] = {(cuuint32_t)inner, (cuuint32_t)(o.mn ? inner : tile)};
+    const cuuint32_t box[2] = {(cuuint32_t)inner, (cuuint32_t)(o.mn ? inner : box_rows)};
     const cuuint32_t ones[2] = {1, 1};
     const CUtensorMapDataType type = dtype == HPF_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == HPF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     const CUresult r = g_encode(tm, type, 2, const_cast<void*>(o.p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -665,21 +770,49 @@ cudaError_t launch_gemm(GemmArgs& g, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, kernel, g);
 }
 
+// Clusters of 1, 2, 4 and 8 CTAs of this kernel's shape that the device holds at a time (one CTA per SM; a cluster stays within a GPC,
+// so of the larger ones fewer fit than the SMs would make: with twice 8 more CTAs than fit, products took 16 us longer).
+struct Fit {
+    int clusters[4];
+};
+cudaError_t how_many_fit(Fit* fit)
+{
+    static PerDevice<Fit> known;
+    return known.get(fit, [](int, Fit* f) {
+        auto* kernel = linear_gemm_kernel<2, __nv_bfloat16, 128, false>;
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        for (int i = 0; i < 4 && e == cudaSuccess; ++i) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(1u << i);
+            cfg.blockDim = dim3(Shape<2, 128>::kThreads);
+            cfg.dynamicSmemBytes = kSmem;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = 1u << i;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&f->clusters[i], kernel, &cfg);
+            if (e == cudaSuccess && f->clusters[i] < 1) f->clusters[i] = 1;
+        }
+        return e;
+    });
+}
 struct Plan {
     int bn, split;
 };
 // Tile width and split of k by a modelled time in clocks: waves of CTAs x (stages a CTA runs through x clocks of a stage's MMAs + what
-// a tile costs besides).  Clocks of one MMA (M = 128): 48 at N = 64, 64 at 128, 128 at 256.
-Plan choose(int64_t M, int64_t N, int k_blocks, int widest, int mmas)
+// a tile costs besides).  Clocks of one MMA (M = 128): 39 at N = 32, 48 at 64, 64 at 128, 128 at 256.
+Plan choose(int64_t lanes, int64_t cols, int k_blocks, int narrowest, int widest, int mmas, const Fit& fit)
 {
-    Plan best{64, 1};
+    Plan best{widest, 1};
     double least = 1e300;
-    for (int bn = widest; bn >= 64; bn /= 2) {
-        const int64_t tiles = ((M + kTileM - 1) / kTileM) * ((N + bn - 1) / bn);
-        const double stage = mmas * (bn == 256 ? 128.0 : bn == 128 ? 64.0 : 48.0);
-        for (int split = 1; split <= kMaxSplit; split *= 2) {
-            if (split > 1 && (k_blocks < 2 * split || tiles * split > 2 * sm_count())) break;
-            const int64_t waves = (tiles * split + sm_count() - 1) / sm_count();
+    for (int bn = widest; bn >= narrowest; bn /= 2) {
+        const int64_t tiles = ((lanes + kTileM - 1) / kTileM) * ((cols + bn - 1) / bn);
+        const double stage = mmas * (bn == 256 ? 128.0 : bn == 128 ? 64.0 : bn == 64 ? 48.0 : 39.0);
+        for (int i = 0, split = 1; split <= kMaxSplit; ++i, split *= 2) {
+            if (split > 1 && (k_blocks < 2 * split || tiles > 2 * fit.clusters[i])) break;
+            const int64_t waves = (tiles + fit.clusters[i] - 1) / fit.clusters[i];
             const double t = waves * (((k_blocks + split - 1) / split) * stage + 6.0 * bn) + 2500.0 + (split > 1 ? 1500.0 : 0.0);
             if (t < least) { least = t; best = Plan{bn, split}; }
         }
@@ -687,40 +820,59 @@ Plan choose(int64_t M, int64_t N, int k_blocks, int widest, int mmas)
     return best;
 }
 
-// out[M][N] = sum_k A B in the operands' type; out_fp32: the result is fp32 whatever that type is
+template <int E, typename T, bool PROMOTE>
+cudaError_t launch_width(GemmArgs& g, int bn, cudaStream_t st)
+{
+    if constexpr (!PROMOTE) {
+        if (bn == 256) return launch_gemm<E, T, 256, PROMOTE>(g, st);
+    }
+    return bn == 128 ? launch_gemm<E, T, 128, PROMOTE>(g, st) : bn == 64 ? launch_gemm<E, T, 64, PROMOTE>(g, st) : launch_gemm<E, T, 32, PROMOTE>(g, st);
+}
+
+constexpr int kFewRows = 64;       // up to here the rows of out are the narrow side of a tile
+
+// out[rows][cols] = sum_k a(row, k) b(col, k); out_fp32: the result is fp32 whatever the operands' type is
 template <int E>
-cudaError_t gemm(GemmArgs& g, const Operand& a, const Operand& b, int64_t M, int64_t N, int64_t K, int32_t dtype, bool out_fp32, cudaStream_t st)
+cudaError_t gemm(GemmArgs& g, Operand a, Operand b, int64_t rows, int64_t cols, int64_t K, int32_t dtype, bool out_fp32, cudaStream_t st)
 {
     const bool promote = dtype == HPF_FP32 || out_fp32;
-    const int k_blocks = (int)((K * E + kRow - 1) / kRow);
-    const Plan plan = choose(M, N, k_blocks, promote ? 128 : 256, E == 4 ? 12 : 4);
-    g.M = (int)M; g.N = (int)N; g.k_blocks = k_blocks; g.split = plan.split;
-    g.tiles_m = (int)((M + kTileM - 1) / kTileM);
-    g.tiles_n = (int)((N + plan.bn - 1) / plan.bn);
+    Fit fit;
+    cudaError_t e = how_many_fit(&fit);
+    if (e != cudaSuccess) return e;
+    const size_t oe = promote ? 4 : 2;
+    g.rows = (int)rows;
+    g.cols = (int)cols;
+    g.wide = aligned16(g.out) && (g.ld * oe) % 16 == 0 && (!g.z || aligned16(g.z)) && (!g.residual || aligned16(g.residual));
+    g.swap = rows <= kFewRows && !a.mn;
+    int64_t lanes = rows, across = cols;
+    if (g.swap) {
+        const Operand o = a; a = b; b = o;
+        lanes = cols;
+        across = rows;
+    }
+    g.k_blocks = (int)((K * E + kRow - 1) / kRow);
+    const Plan plan = choose(lanes, across, g.k_blocks, g.swap ? 32 : 64, g.swap ? (across <= 32 ? 32 : 64) : promote ? 128 : 256, E == 4 ? 12 : 4, fit);
+    g.split = plan.split;
+    g.tiles_m = (int)((lanes + kTileM - 1) / kTileM);
+    g.tiles_n = (int)((across + plan.bn - 1) / plan.bn);
     g.a_mn = a.mn; g.b_mn = b.mn;
+    g.a_box = (int)(lanes < kTileM ? (lanes + 7) / 8 * 8 : kTileM);
+    g.b_box = (int)(across < plan.bn ? (across + 7) / 8 * 8 : plan.bn);
     const uint32_t fmt = dtype == HPF_FP32 ? 2u : dtype == HPF_BF16 ? 1u : 0u;
     g.idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((a.mn ? 1u : 0u) << 15) | ((b.mn ? 1u : 0u) << 16) | ((uint32_t)(plan.bn >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
-    const size_t oe = promote ? 4 : 2;
-    g.wide = aligned16(g.out) && (g.ld * oe) % 16 == 0 && (!g.z || aligned16(g.z)) && (!g.residual || aligned16(g.residual));
-    cudaError_t e = make_map<E>(&g.ta, a, dtype, kTileM);
-    if (e == cudaSuccess) e = make_map<E>(&g.tb, b, dtype, plan.bn);
+    e = make_map<E>(&g.ta, a, dtype, g.a_box);
+    if (e == cudaSuccess) e = make_map<E>(&g.tb, b, dtype, g.b_box);
     if (e != cudaSuccess) return e;
     if constexpr (E == 4) {
-        return plan.bn == 128 ? launch_gemm<4, float, 128, true>(g, st) : launch_gemm<4, float, 64, true>(g, st);
+        return launch_width<4, float, true>(g, plan.bn, st);
     } else {
-        if (out_fp32) return plan.bn == 128 ? launch_gemm<2, float, 128, true>(g, st) : launch_gemm<2, float, 64, true>(g, st);
-        if (dtype == HPF_BF16)
-            return plan.bn == 256   ? launch_gemm<2, __nv_bfloat16, 256, false>(g, st)
-                   : plan.bn == 128 ? launch_gemm<2, __nv_bfloat16, 128, false>(g, st)
-                                    : launch_gemm<2, __nv_bfloat16, 64, false>(g, st);
-        return plan.bn == 256   ? launch_gemm<2, __half, 256, false>(g, st)
-               : plan.bn == 128 ? launch_gemm<2, __half, 128, false>(g, st)
-                                : launch_gemm<2, __half, 64, false>(g, st);
+        if (out_fp32) return launch_width<2, float, true>(g, plan.bn, st);
+        return dtype == HPF_BF16 ? launch_width<2, __nv_bfloat16, false>(g, plan.bn, st) : launch_width<2, __half, false>(g, plan.bn, st);
     }
 }
-cudaError_t gemm_any(GemmArgs& g, const Operand& a, const Operand& b, int64_t M, int64_t N, int64_t K, int32_t dtype, bool out_fp32, cudaStream_t st)
+cudaError_t gemm_any(GemmArgs& g, const Operand& a, const Operand& b, int64_t rows, int64_t cols, int64_t K, int32_t dtype, bool out_fp32, cudaStream_t st)
 {
-    return dtype == HPF_FP32 ? gemm<4>(g, a, b, M, N, K, dtype, out_fp32, st) : gemm<2>(g, a, b, M, N, K, dtype, out_fp32, st);
+    return dtype == HPF_FP32 ? gemm<4>(g, a, b, rows, cols, K, dtype, out_fp32, st) : gemm<2>(g, a, b, rows, cols, K, dtype, out_fp32, st);
 }
 
 cudaError_t repack(const void* in, void* out, int64_t rows, int n, int64_t ld, int64_t ld_out, int e, cudaStream_t st)
