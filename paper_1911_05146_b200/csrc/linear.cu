@@ -224,6 +224,18 @@ __device__ __forceinline__ Tile tile_at(int t, int tiles_m, int tiles_n)
 // Where 16-byte unit u of row r of a 32 x 32 block lies: units of a row are spread so that both the writers (a row per lane) and the
 // readers (a few rows at a time) touch all banks.
 __device__ __forceinline__ uint32_t unit_at(uint32_t block, int r, int u) { return block + r * 128 + ((u ^ (r & 7)) << 4); }
+__device__ __forceinline__ float4 shared_get4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ float shared_get(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+    return v;
+}
 // A lane's 32 values as row `lane` of the block, or (swapped) as column `lane`.
 __device__ __forceinline__ void block_put(uint32_t block, int lane, const float* v, int swap)
 {
@@ -237,122 +249,144 @@ __device__ __forceinline__ void block_put(uint32_t block, int lane, const float*
         for (int j = 0; j < 32; ++j) asm volatile("st.shared.f32 [%0], %1;" ::"r"(unit_at(block, j, lane >> 2) + (lane & 3) * 4), "f"(v[j]) : "memory");
     }
 }
-__device__ __forceinline__ float4 shared_get4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-    return v;
-}
-__device__ __forceinline__ float shared_get(uint32_t addr)
-{
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr));
-    return v;
-}
 __device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank)
 {
     uint32_t there;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
     return there;
 }
-__device__ __forceinline__ float4 cluster_get4(uint32_t addr)
+// The same towards the CTAs of a cluster.  A tile's quarter blocks (8 rows x 32 columns, 1 KB) are dealt out to the ranks; the owner
+// keeps the `split` versions of a quarter side by side.  Stores to another CTA need no answer: reading the partial tiles over from their
+// owners instead left a warp waiting 5 us for a 128 x 128 tile of four.
+__device__ __forceinline__ void block_push(uint32_t slots, int block, int lane, const float* v, int swap, int split, int rank, int rows)
 {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-    return v;
-}
-// the sum of the cluster's values at one place, in rank order; all loads are under way before the first is needed
-__device__ __forceinline__ float4 cluster_sum4(uint32_t addr, int split)
-{
-    float4 part[kMaxSplit];
+    if (!swap) {
+        const int i = block * 4 + (lane >> 3);
+        const uint32_t to = at_rank(slots + ((i & -split) + rank) * 1024, i & (split - 1));
+        if (lane < rows) {
 #pragma unroll
-    for (int k = 0; k < kMaxSplit; ++k)
-        if (k < split) part[k] = cluster_get4(at_rank(addr, k));
-    float4 s = part[0];
+            for (int u = 0; u < 8; ++u)
+                asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(unit_at(to, lane & 7, u)), "f"(v[4 * u]), "f"(v[4 * u + 1]), "f"(v[4 * u + 2]), "f"(v[4 * u + 3])
+                             : "memory");
+        }
+    } else {
 #pragma unroll
-    for (int k = 1; k < kMaxSplit; ++k)
-        if (k < split) { s.x += part[k].x; s.y += part[k].y; s.z += part[k].z; s.w += part[k].w; }
-    return s;
+        for (int j = 0; j < 32; ++j) {
+            const int i = block * 4 + (j >> 3);
+            const uint32_t to = at_rank(slots + ((i & -split) + rank) * 1024, i & (split - 1));
+            if (j < rows) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(unit_at(to, j & 7, lane >> 2) + (lane & 3) * 4), "f"(v[j]) : "memory");
+        }
+    }
 }
 
-// The last steps on V values of one row of out that start at column col: bias, activation, residual, one rounding.
-template <typename T>
-__device__ __forceinline__ void finish_wide(const GemmArgs& p, float* v, const float* bias, int row, int col)
+__device__ __forceinline__ void cluster_barrier()
 {
-    constexpr int V = Pack<T>::V;
-    const int64_t at = row * p.ld + col;
-    uint4 res;
-    if (p.residual) res = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.residual) + at);
-#pragma unroll
-    for (int j = 0; j < V; ++j) v[j] += bias[j];
-    if (p.z) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.z) + at) = Pack<T>::pack(v);
-    if (p.act != HPF_ACT_NONE) activate<V>(v, p.act);
-    if (p.residual) {
-        float f[V];
-        Pack<T>::unpack(res, f);
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] += f[j];
-    }
-    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + at) = Pack<T>::pack(v);
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-template <typename T>
-__device__ __forceinline__ void finish_one(const GemmArgs& p, float v, float bias, int row, int col)
-{
-    const int64_t at = row * p.ld + col;
-    v += bias;
-    if (p.z) reinterpret_cast<T*>(p.z)[at] = Pack<T>::put(v);
-    if (p.act != HPF_ACT_NONE) activate<1>(&v, p.act);
-    if (p.residual) v += Pack<T>::get(reinterpret_cast<const T*>(p.residual)[at]);
-    reinterpret_cast<T*>(p.out)[at] = Pack<T>::put(v);
-}
-// One warp finishes rows [from, to) of the 32 x 32 block of out at (row0, col0) whose fp32 sums lie in shared memory (SPLIT: of all CTAs
-// of the cluster).  16 bytes of a row per lane where rows lie on 16-byte boundaries, else a column per lane: either way an access is
-// whole sectors.  The loops stay rolled: unrolled, this code no longer fitted the instruction
-// caches and a 128 x 128 tile took 4 us to write out.
-template <typename T, bool SPLIT>
-__device__ __forceinline__ void finish_block(const GemmArgs& p, uint32_t block, int row0, int col0, int from, int to, int lane)
+
+// One warp finishes ROWS_IN rows of out from (row0, col0) on, 32 columns wide, whose fp32 sums lie in shared memory: bias, activation,
+// residual, one rounding.  `split` versions of the sums, 1 KB apart, are added up in order.  16 bytes of a row per lane where rows lie on
+// 16-byte boundaries, else a column per lane: either way an access is whole sectors.  Four (eight) accesses of each kind are under
+// way together; not more, since code unrolled further no longer fitted the instruction caches.
+template <typename T, int ROWS_IN>
+__device__ __forceinline__ void finish_rows(const GemmArgs& p, uint32_t block, int split, int row0, int col0, int lane)
 {
     constexpr int V = Pack<T>::V, PER_ROW = 32 / V, ROWS = 32 / PER_ROW;
-    const int rows = min(to, p.rows - row0);
-    if (rows <= from || col0 >= p.cols) return;
+    const int rows = min(ROWS_IN, p.rows - row0);
+    if (rows <= 0 || col0 >= p.cols) return;
     if (p.wide && col0 + 32 <= p.cols) {
-        const int c = (lane % PER_ROW) * V, col = col0 + c;
+        constexpr int PASSES = ROWS_IN / ROWS, B = PASSES < 4 ? PASSES : 4;
+        const int c = lane % PER_ROW, col = col0 + c * V;
         float bias[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) bias[j] = 0.f;
         if (p.bias) {
 #pragma unroll
             for (int j = 0; j < V; ++j) bias[j] = Pack<T>::get(reinterpret_cast<const T*>(p.bias)[col + j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) bias[j] = 0.f;
         }
 #pragma unroll 1
-        for (int r = from + lane / PER_ROW; r < rows; r += ROWS) {
-            float v[V];
+        for (int g = 0; g < PASSES; g += B) {
+            float v[B * V];
+            uint4 res[B];
+            const int r0 = g * ROWS + lane / PER_ROW;
+            const int64_t at = (int64_t)(row0 + r0) * p.ld + col, step = ROWS * p.ld;
+            if (p.residual) {
 #pragma unroll
-            for (int h = 0; h < V / 4; ++h) {
-                const uint32_t at = unit_at(block, r, (lane % PER_ROW) * (V / 4) + h);
-                const float4 s = SPLIT ? cluster_sum4(at, p.split) : shared_get4(at);
-                v[4 * h] = s.x; v[4 * h + 1] = s.y; v[4 * h + 2] = s.z; v[4 * h + 3] = s.w;
+                for (int i = 0; i < B; ++i)
+                    if (r0 + i * ROWS < rows) res[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.residual) + at + i * step);
             }
-            finish_wide<T>(p, v, bias, row0 + r, col);
+#pragma unroll
+            for (int i = 0; i < B; ++i)
+#pragma unroll
+                for (int h = 0; h < V / 4; ++h) {
+                    const float4 s = shared_get4(unit_at(block, r0 + i * ROWS, c * (V / 4) + h));
+                    float* f = v + i * V + h * 4;
+                    f[0] = s.x; f[1] = s.y; f[2] = s.z; f[3] = s.w;
+                }
+            for (int k = 1; k < split; ++k) {
+#pragma unroll
+                for (int i = 0; i < B; ++i)
+#pragma unroll
+                    for (int h = 0; h < V / 4; ++h) {
+                        const float4 s = shared_get4(unit_at(block + k * 1024, r0 + i * ROWS, c * (V / 4) + h));
+                        float* f = v + i * V + h * 4;
+                        f[0] += s.x; f[1] += s.y; f[2] += s.z; f[3] += s.w;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < B * V; ++i) v[i] += bias[i % V];
+            if (p.z) {
+#pragma unroll
+                for (int i = 0; i < B; ++i)
+                    if (r0 + i * ROWS < rows) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.z) + at + i * step) = Pack<T>::pack(v + i * V);
+            }
+            if (p.act != HPF_ACT_NONE) activate<B * V>(v, p.act);
+            if (p.residual) {
+#pragma unroll
+                for (int i = 0; i < B; ++i) {
+                    float f[V];
+                    Pack<T>::unpack(res[i], f);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) v[i * V + j] += f[j];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < B; ++i)
+                if (r0 + i * ROWS < rows) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + at + i * step) = Pack<T>::pack(v + i * V);
         }
     } else if (col0 + lane < p.cols) {
         const int col = col0 + lane;
         const float bias = p.bias ? Pack<T>::get(reinterpret_cast<const T*>(p.bias)[col]) : 0.f;
 #pragma unroll 1
-        for (int r = from; r < rows; ++r) {
-            const uint32_t at = unit_at(block, r, lane >> 2) + (lane & 3) * 4;
-            float v = 0.f;
-            if (SPLIT) {
-                for (int k = 0; k < p.split; ++k) {
-                    float o;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o) : "r"(at_rank(at, k)));
-                    v += o;
-                }
-            } else {
-                v = shared_get(at);
+        for (int g = 0; g < rows; g += 8) {
+            float v[8], res[8];
+            const int64_t at = (int64_t)(row0 + g) * p.ld + col;
+            if (p.residual) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (g + i < rows) res[i] = Pack<T>::get(reinterpret_cast<const T*>(p.residual)[at + i * p.ld]);
             }
-            finish_one<T>(p, v, bias, row0 + r, col);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = shared_get(unit_at(block, g + i, lane >> 2) + (lane & 3) * 4);
+            for (int k = 1; k < split; ++k) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += shared_get(unit_at(block + k * 1024, g + i, lane >> 2) + (lane & 3) * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += bias;
+            if (p.z) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (g + i < rows) reinterpret_cast<T*>(p.z)[at + i * p.ld] = Pack<T>::put(v[i]);
+            }
+            if (p.act != HPF_ACT_NONE) activate<8>(v, p.act);
+            if (p.residual) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += res[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (g + i < rows) reinterpret_cast<T*>(p.out)[at + i * p.ld] = Pack<T>::put(v[i]);
         }
     }
 }
@@ -389,6 +423,10 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
     const int first = (int)(blockIdx.x / (unsigned)split), step = split > 1 ? tiles : (int)gridDim.x;      // a cluster has one tile
     const int kb0 = (int)((long long)p.k_blocks * rank / split), kb1 = (int)((long long)p.k_blocks * (rank + 1) / split);
 
+    if (threadIdx.x == 32) {
+        prefetch_tmap(&p.ta);
+        prefetch_tmap(&p.tb);
+    }
     if (threadIdx.x == 0) {
         s_abort = 0;
         for (int i = 0; i < STAGES; ++i) {
@@ -411,8 +449,6 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
 
     if (warp == 0) {
         if (elect_one()) {
-            prefetch_tmap(&p.ta);
-            prefetch_tmap(&p.tb);
             const uint32_t bytes = (p.a_mn ? S::kA : p.a_box * kRow) + (p.b_mn ? S::kB : p.b_box * kRow);
             int it = 0;
             bool live = true;
@@ -494,28 +530,25 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
         }
         __syncwarp();
     } else if (warp >= 4 && warp < 4 + kOutWarps) {
-        const int quad = warp & 3, half = (warp - 4) >> 2;
         constexpr int BLOCKS = BN / 64 > 0 ? BN / 64 : 1;     // blocks of 32 columns of this warp (BN = 32: of the first four warps)
+        const int quad = warp & 3, half = (warp - 4) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t mine = staging + (warp - 4) * kBlock;
+        float acc[PROMOTE ? BLOCKS : 1][32];
         int chunk = 0;
         bool live = true;
         for (int t = first; live && t < tiles; t += step) {
             const Tile tile = tile_at(t, p.tiles_m, p.tiles_n);
             // block c of the tile, once its sums are in the warp's registers
             const auto hand_over = [&](int c, const float* v) {
-                if (split > 1) {
-                    block_put(ring + (c * 4 + quad) * kBlock, lane, v, p.swap);
-                } else {
-                    block_put(mine, lane, v, p.swap);
-                    __syncwarp();
-                    const int at_m = tile.m * kTileM + quad * 32, at_n = tile.n * BN + c * 32;
-                    finish_block<T, false>(p, mine, p.swap ? at_n : at_m, p.swap ? at_m : at_n, 0, 32, lane);
-                    __syncwarp();
-                }
+                const int at_m = tile.m * kTileM + quad * 32, at_n = tile.n * BN + c * 32;
+                const int row0 = p.swap ? at_n : at_m, col0 = p.swap ? at_m : at_n;
+                block_put(mine, lane, v, p.swap);
+                __syncwarp();
+                finish_rows<T, 32>(p, mine, 1, row0, col0, lane);
+                __syncwarp();
             };
             if constexpr (PROMOTE) {
-                float acc[BLOCKS][32];
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
@@ -540,7 +573,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                     if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
                 }
                 if (!live) break;
-                if (BN > 32 || half == 0) {
+                if (split == 1 && (BN > 32 || half == 0)) {
 #pragma unroll
                     for (int b = 0; b < BLOCKS; ++b) hand_over(half * BLOCKS + b, acc[b]);
                 }
@@ -551,6 +584,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                 if (!live) { report(p.status, 43); break; }
                 tc_fence_after();
                 ++chunk;
+                if (split > 1) break;                          // the sums are fetched once the whole cluster is done
 #pragma unroll 1
                 for (int b = 0; b < BLOCKS; ++b) {
                     const int c = half * BLOCKS + b;
@@ -562,6 +596,30 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                         if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
                     }
                     if (BN > 32 || half == 0) hand_over(c, v);
+                }
+            }
+        }
+        if (split > 1) {
+            cluster_barrier();                                 // every product of the cluster is done: the rings are free
+            if (live && (BN > 32 || half == 0)) {
+                const Tile tile = tile_at(first, p.tiles_m, p.tiles_n);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    const int c = half * BLOCKS + b, at_m = tile.m * kTileM + quad * 32, at_n = tile.n * BN + c * 32;
+                    float v[32];
+                    if constexpr (!PROMOTE) tmem_ld32(tmem + lanes + c * 32, v);
+                    const float* sums = v;
+                    if constexpr (PROMOTE) sums = acc[b];
+                    block_push(ring, c * 4 + quad, lane, sums, p.swap, split, rank, p.rows - (p.swap ? at_n : at_m));
+                }
+            }
+            cluster_barrier();
+            if (live) {
+                const Tile tile = tile_at(first, p.tiles_m, p.tiles_n);
+                for (int i = warp - 4; i * split + rank < BN / 32 * 16; i += kOutWarps) {
+                    const int item = i * split + rank, u = item >> 2;
+                    const int at_m = tile.m * kTileM + (u & 3) * 32, at_n = tile.n * BN + (u >> 2) * 32;
+                    finish_rows<T, 8>(p, ring + i * split * 1024, split, (p.swap ? at_n : at_m) + (item & 3) * 8, p.swap ? at_m : at_n, lane);
                 }
             }
         }
@@ -598,22 +656,13 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
         }
     }
 
-    tc_fence_before();
-    if (split > 1) {
-        // every product of the cluster is done, so the rings hold partial tiles only
-        cg::this_cluster().sync();
-        if (warp >= 4 && warp < 4 + kOutWarps && !*abort_flag) {
-            const Tile tile = tile_at(first, p.tiles_m, p.tiles_n);
-            // quarters of blocks, 8 rows each, dealt out to the ranks and their warps
-            for (int i = (warp - 4) * split + rank; i < BN / 32 * 16; i += kOutWarps * split) {
-                const int u = i >> 2, from = (i & 3) * 8, at_m = tile.m * kTileM + (u & 3) * 32, at_n = tile.n * BN + (u >> 2) * 32;
-                finish_block<T, true>(p, ring + u * kBlock, p.swap ? at_n : at_m, p.swap ? at_m : at_n, from, from + 8, lane);
-            }
-        }
-        cg::this_cluster().sync();
-    } else {
-        __syncthreads();
+    if (split > 1 && !(warp >= 4 && warp < 4 + kOutWarps)) {
+        __syncwarp();
+        cluster_barrier();
+        cluster_barrier();
     }
+    tc_fence_before();
+    __syncthreads();
     tc_fence_after();
     if (warp == 2) tmem_dealloc(tmem, 2 * BN);
 }
@@ -801,15 +850,17 @@ cudaError_t how_many_fit(Fit* fit)
 struct Plan {
     int bn, split;
 };
-// Tile width and split of k by a modelled time in clocks: waves of CTAs x (stages a CTA runs through x clocks of a stage's MMAs + what
-// a tile costs besides).  Clocks of one MMA (M = 128): 39 at N = 32, 48 at 64, 64 at 128, 128 at 256.
+// Tile width and split of k by a modelled time in clocks: waves of CTAs x (stages a CTA runs through x clocks of a stage + what a tile
+// costs besides).  A stage takes its MMAs (M = 128: 39 clocks at N = 32, 48 at 64, 64 at 128, 128 at 256) or its copies at 48 bytes a
+// clock, what L2 gave every SM at once, whichever is longer.
 Plan choose(int64_t lanes, int64_t cols, int k_blocks, int narrowest, int widest, int mmas, const Fit& fit)
 {
     Plan best{widest, 1};
     double least = 1e300;
     for (int bn = widest; bn >= narrowest; bn /= 2) {
         const int64_t tiles = ((lanes + kTileM - 1) / kTileM) * ((cols + bn - 1) / bn);
-        const double stage = mmas * (bn == 256 ? 128.0 : bn == 128 ? 64.0 : bn == 64 ? 48.0 : 39.0);
+        const double products = mmas * (bn == 256 ? 128.0 : bn == 128 ? 64.0 : bn == 64 ? 48.0 : 39.0), copies = (kTileM + bn) * kRow / 48.0;
+        const double stage = products > copies ? products : copies;
         for (int i = 0, split = 1; split <= kMaxSplit; ++i, split *= 2) {
             if (split > 1 && (k_blocks < 2 * split || tiles > 2 * fit.clusters[i])) break;
             const int64_t waves = (tiles + fit.clusters[i] - 1) / fit.clusters[i];
@@ -889,8 +940,9 @@ cudaError_t launch_dz(DzArgs& a, cudaStream_t st)
 {
     const int cols = 128 / sizeof(T);
     const bool wide = aligned16(a.dy) && (a.ld * sizeof(T)) % 16 == 0 && (a.act == HPF_ACT_NONE || aligned16(a.z));
-    const int64_t want = (a.rows + 63) / 64;
-    a.parts = (int)(want < 1 ? 1 : want > 8 ? 8 : want);
+    // one CTA goes down up to 256 rows by itself: joining a cluster's sums takes longer than that
+    const int64_t want = (a.rows + 255) / 256;
+    a.parts = (int)(want > 8 ? 8 : want);
     auto* kernel = wide ? linear_dz_kernel<T, true> : linear_dz_kernel<T, false>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((a.n + cols - 1) / cols * a.parts));
