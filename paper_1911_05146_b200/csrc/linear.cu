@@ -36,12 +36,12 @@ constexpr int kRow = 128;                      // bytes of k (or of m / n) in a 
 constexpr int kRing = 192 * 1024;              // bytes of the ring of stages
 constexpr int kBlock = 4096;                   // a 32 x 32 block of fp32 on its way out
 constexpr int kOutWarps = 8;
-constexpr int kSmem = kRing + kOutWarps * kBlock + 1024 + 512;
+constexpr int kSmem = kRing + kOutWarps * (kBlock + 128) + 1024;
 constexpr int kMaxStages = 8;
 constexpr int kMaxSplit = 8;
 
 struct GemmArgs {
-    CUtensorMap ta, tb;
+    CUtensorMap ta, tb, t_out, t_z;            // the last two where `copy_out`
     int rows, cols;                            // of out
     int k_blocks, tiles_m, tiles_n, split;
     int swap;                                  // few rows: a tile's 128 lanes are columns of out, its BN columns rows of out
@@ -49,6 +49,7 @@ struct GemmArgs {
     int a_box, b_box;                          // rows of m / n that a k-contiguous stage is filled with (the rest is never looked at)
     uint32_t idesc;
     int act, wide;                             // wide: every output and the residual take 16-byte accesses
+    int copy_out;                              // tiles leave by tensor copies (wide, whole k in one CTA, rows of out in the lanes)
     void *out, *z;
     const void *bias, *residual;
     int64_t ld;                                // of out, z and residual
@@ -277,6 +278,90 @@ __device__ __forceinline__ void block_push(uint32_t slots, int block, int lane, 
             if (j < rows) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(unit_at(to, j & 7, lane >> 2) + (lane & 3) * 4), "f"(v[j]) : "memory");
         }
     }
+}
+
+__device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tmap), "r"(src), "r"(c0), "r"(c1) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// all but the last N copies out have read their shared memory
+template <int N>
+__device__ __forceinline__ void tma_store_wait()
+{
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+// A 32 x 32 block on its way out by a tensor copy: a lane holds row `lane`; 16-byte units are spread as the copy's swizzle has them.
+template <typename T>
+struct Slab {
+    static constexpr int kBytes = 32 * 32 * sizeof(T), kSlabs = kBlock / kBytes;
+    static __device__ __forceinline__ void put(uint32_t slab, int lane, const float* v)
+    {
+        constexpr int V = Pack<T>::V;
+#pragma unroll
+        for (int u = 0; u < 32 / V; ++u) {
+            const uint32_t at = sizeof(T) == 2 ? slab + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4) : slab + lane * 128 + ((u ^ (lane & 7)) << 4);
+            const uint4 w = Pack<T>::pack(v + u * V);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+        }
+    }
+};
+// One warp sends the block of out at (row0, col0) off, `n` counting its copies.  Rows and columns beyond out are cut off by the copy.
+template <typename T>
+__device__ __forceinline__ void send_slab(const CUtensorMap* map, uint32_t slabs, int* n, const float* v, int row0, int col0, int lane)
+{
+    const uint32_t slab = slabs + (*n % Slab<T>::kSlabs) * Slab<T>::kBytes;
+    ++*n;
+    if (lane == 0) tma_store_wait<Slab<T>::kSlabs - 1>();
+    __syncwarp();
+    Slab<T>::put(slab, lane, v);
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) tma_store_2d(map, slab, col0, row0);
+}
+template <typename T>
+__device__ __forceinline__ void send_block(const GemmArgs& p, uint32_t slabs, uint32_t s_bias, int* n, float* v, int row0, int col0, int lane)
+{
+    constexpr int V = Pack<T>::V;
+    if (row0 >= p.rows || col0 >= p.cols) return;
+    const T* r = reinterpret_cast<const T*>(p.residual) + (int64_t)(row0 + lane) * p.ld + col0;
+    const auto residual = [&](int u) {                       // 16 bytes of it; a last piece of fewer than V columns is read one by one
+        if (row0 + lane >= p.rows || col0 + u * V >= p.cols) return make_uint4(0, 0, 0, 0);
+        if (col0 + (u + 1) * V <= p.cols) return *reinterpret_cast<const uint4*>(r + u * V);
+        float f[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = col0 + u * V + j < p.cols ? Pack<T>::get(r[u * V + j]) : 0.f;
+        return Pack<T>::pack(f);
+    };
+    constexpr int AHEAD = sizeof(T) == 2 ? 32 / V : 1;       // fetched before the rest is done, where registers allow
+    uint4 res[AHEAD];
+    if (AHEAD > 1 && p.residual) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) res[u] = residual(u);
+    }
+    if (p.bias) {
+        const float b = col0 + lane < p.cols ? Pack<T>::get(reinterpret_cast<const T*>(p.bias)[col0 + lane]) : 0.f;
+        __syncwarp();
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(s_bias + lane * 4), "f"(b) : "memory");
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float4 s = shared_get4(s_bias + u * 16);
+            v[4 * u] += s.x; v[4 * u + 1] += s.y; v[4 * u + 2] += s.z; v[4 * u + 3] += s.w;
+        }
+    }
+    if (p.z) send_slab<T>(&p.t_z, slabs, n, v, row0, col0, lane);
+    if (p.act != HPF_ACT_NONE) activate<32>(v, p.act);
+    if (p.residual) {
+#pragma unroll
+        for (int u = 0; u < 32 / V; ++u) {
+            float f[V];
+            Pack<T>::unpack(AHEAD > 1 ? res[u % AHEAD] : residual(u), f);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[u * V + j] += f[j];
+        }
+    }
+    send_slab<T>(&p.t_out, slabs, n, v, row0, col0, lane);
 }
 
 __device__ __forceinline__ void cluster_barrier()
@@ -534,15 +619,20 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
         const int quad = warp & 3, half = (warp - 4) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t mine = staging + (warp - 4) * kBlock;
+        const uint32_t bias = staging + kOutWarps * kBlock + (warp - 4) * 128;
         float acc[PROMOTE ? BLOCKS : 1][32];
-        int chunk = 0;
+        int chunk = 0, sent = 0;
         bool live = true;
         for (int t = first; live && t < tiles; t += step) {
             const Tile tile = tile_at(t, p.tiles_m, p.tiles_n);
             // block c of the tile, once its sums are in the warp's registers
-            const auto hand_over = [&](int c, const float* v) {
+            const auto hand_over = [&](int c, float* v) {
                 const int at_m = tile.m * kTileM + quad * 32, at_n = tile.n * BN + c * 32;
                 const int row0 = p.swap ? at_n : at_m, col0 = p.swap ? at_m : at_n;
+                if (p.copy_out) {
+                    send_block<T>(p, mine, bias, &sent, v, at_m, at_n, lane);
+                    return;
+                }
                 block_put(mine, lane, v, p.swap);
                 __syncwarp();
                 finish_rows<T, 32>(p, mine, 1, row0, col0, lane);
@@ -599,6 +689,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                 }
             }
         }
+        if (p.copy_out && lane == 0) tma_store_wait<0>();
         if (split > 1) {
             cluster_barrier();                                 // every product of the cluster is done: the rings are free
             if (live && (BN > 32 || half == 0)) {
@@ -796,6 +887,19 @@ cudaError_t make_map(CUtensorMap* tm, const Operand& o, int32_t dtype, int box_r
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+// map of an output: copies of 32 x 32 blocks
+template <typename T>
+cudaError_t make_out_map(CUtensorMap* tm, void* out, int64_t rows, int64_t cols, int64_t ld, int32_t dtype)
+{
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)(ld * sizeof(T))};
+    const cuuint32_t box[2] = {32, 32}, ones[2] = {1, 1};
+    const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == HPF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const CUresult r = g_encode(tm, type, 2, out, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                sizeof(T) == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 template <int E, typename T, int BN, bool PROMOTE>
 cudaError_t launch_gemm(GemmArgs& g, cudaStream_t st)
 {
@@ -872,8 +976,14 @@ Plan choose(int64_t lanes, int64_t cols, int k_blocks, int narrowest, int widest
 }
 
 template <int E, typename T, bool PROMOTE>
-cudaError_t launch_width(GemmArgs& g, int bn, cudaStream_t st)
+cudaError_t launch_width(GemmArgs& g, int bn, int32_t dtype, cudaStream_t st)
 {
+    g.copy_out = g.wide && g.split == 1 && !g.swap;
+    if (g.copy_out) {
+        cudaError_t e = make_out_map<T>(&g.t_out, g.out, g.rows, g.cols, g.ld, dtype);
+        if (e == cudaSuccess && g.z) e = make_out_map<T>(&g.t_z, g.z, g.rows, g.cols, g.ld, dtype);
+        if (e != cudaSuccess) return e;
+    }
     if constexpr (!PROMOTE) {
         if (bn == 256) return launch_gemm<E, T, 256, PROMOTE>(g, st);
     }
@@ -915,10 +1025,10 @@ cudaError_t gemm(GemmArgs& g, Operand a, Operand b, int64_t rows, int64_t cols, 
     if (e == cudaSuccess) e = make_map<E>(&g.tb, b, dtype, g.b_box);
     if (e != cudaSuccess) return e;
     if constexpr (E == 4) {
-        return launch_width<4, float, true>(g, plan.bn, st);
+        return launch_width<4, float, true>(g, plan.bn, dtype, st);
     } else {
-        if (out_fp32) return launch_width<2, float, true>(g, plan.bn, st);
-        return dtype == HPF_BF16 ? launch_width<2, __nv_bfloat16, false>(g, plan.bn, st) : launch_width<2, __half, false>(g, plan.bn, st);
+        if (out_fp32) return launch_width<2, float, true>(g, plan.bn, dtype, st);
+        return dtype == HPF_BF16 ? launch_width<2, __nv_bfloat16, false>(g, plan.bn, dtype, st) : launch_width<2, __half, false>(g, plan.bn, dtype, st);
     }
 }
 cudaError_t gemm_any(GemmArgs& g, const Operand& a, const Operand& b, int64_t rows, int64_t cols, int64_t K, int32_t dtype, bool out_fp32, cudaStream_t st)
