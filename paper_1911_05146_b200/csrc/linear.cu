@@ -93,8 +93,22 @@ __device__ __forceinline__ uint64_t desc_mn16(uint32_t addr, uint32_t block_byte
 
 // ---- element types ----------------------------------------------------------------------------------------------------
 template <typename T> struct Pack;
+__device__ __forceinline__ uint16_t shared_u16(uint32_t addr)
+{
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ uint32_t shared_u32(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+    return v;
+}
 template <> struct Pack<float> {
     static constexpr int V = 4;
+    using Word = uint32_t;
+    static __device__ __forceinline__ Word shared_word(uint32_t at) { return shared_u32(at); }
     static __device__ __forceinline__ void unpack(const uint4& r, float* f)
     {
         f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
@@ -108,6 +122,8 @@ template <> struct Pack<float> {
 };
 template <> struct Pack<__nv_bfloat16> {
     static constexpr int V = 8;
+    using Word = uint16_t;
+    static __device__ __forceinline__ Word shared_word(uint32_t at) { return shared_u16(at); }
     static __device__ __forceinline__ void unpack(const uint4& r, float* f)
     {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
@@ -125,6 +141,8 @@ template <> struct Pack<__nv_bfloat16> {
 };
 template <> struct Pack<__half> {
     static constexpr int V = 8;
+    using Word = uint16_t;
+    static __device__ __forceinline__ Word shared_word(uint32_t at) { return shared_u16(at); }
     static __device__ __forceinline__ void unpack(const uint4& r, float* f)
     {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
@@ -319,6 +337,38 @@ __device__ __forceinline__ void send_slab(const CUtensorMap* map, uint32_t slabs
     __syncwarp();
     if (lane == 0) tma_store_2d(map, slab, col0, row0);
 }
+// The same where rows of out are off 16-byte boundaries: a row at a time, a column per lane.
+template <typename T>
+__device__ __forceinline__ void store_slab(void* out, const GemmArgs& p, uint32_t slab, const float* v, int row0, int col0, int lane)
+{
+    using Word = typename Pack<T>::Word;
+    constexpr int UNIT = 16 / (int)sizeof(T), PITCH = 32 * (int)sizeof(T);
+    __syncwarp();
+    Slab<T>::put(slab, lane, v);
+    __syncwarp();
+    if (col0 + lane >= p.cols) return;
+    uint32_t at[8];                                          // of the lane's value in rows 0 .. 7; the pattern repeats
+#pragma unroll
+    for (int i = 0; i < 8; ++i) at[i] = slab + i * PITCH + (((lane / UNIT) ^ (sizeof(T) == 2 ? (i >> 1) & 3 : i)) << 4) + (lane % UNIT) * (int)sizeof(T);
+    Word* q = reinterpret_cast<Word*>(out) + (int64_t)row0 * p.ld + col0 + lane;
+    const int rows = min(32, p.rows - row0);
+#pragma unroll 1
+    for (int g = 0; g < rows; g += 8) {
+        Word w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = Pack<T>::shared_word(at[i] + g * PITCH);
+        if (g + 8 <= rows) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i, q += p.ld) *q = w[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i, q += p.ld)
+                if (g + i < rows) *q = w[i];
+        }
+    }
+}
+// One warp finishes the block of out at (row0, col0), a row per lane: bias, activation, residual (where rows lie on 16-byte boundaries), one
+// rounding.
 template <typename T>
 __device__ __forceinline__ void send_block(const GemmArgs& p, uint32_t slabs, uint32_t s_bias, int* n, float* v, int row0, int col0, int lane)
 {
@@ -350,7 +400,10 @@ __device__ __forceinline__ void send_block(const GemmArgs& p, uint32_t slabs, ui
             v[4 * u] += s.x; v[4 * u + 1] += s.y; v[4 * u + 2] += s.z; v[4 * u + 3] += s.w;
         }
     }
-    if (p.z) send_slab<T>(&p.t_z, slabs, n, v, row0, col0, lane);
+    if (p.z) {
+        if (p.copy_out) send_slab<T>(&p.t_z, slabs, n, v, row0, col0, lane);
+        else store_slab<T>(p.z, p, slabs, v, row0, col0, lane);
+    }
     if (p.act != HPF_ACT_NONE) activate<32>(v, p.act);
     if (p.residual) {
 #pragma unroll
@@ -361,7 +414,8 @@ __device__ __forceinline__ void send_block(const GemmArgs& p, uint32_t slabs, ui
             for (int j = 0; j < V; ++j) v[u * V + j] += f[j];
         }
     }
-    send_slab<T>(&p.t_out, slabs, n, v, row0, col0, lane);
+    if (p.copy_out) send_slab<T>(&p.t_out, slabs, n, v, row0, col0, lane);
+    else store_slab<T>(p.out, p, slabs, v, row0, col0, lane);
 }
 
 __device__ __forceinline__ void cluster_barrier()
@@ -530,6 +584,8 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
+    pdl_launch_dependents();
+    pdl_wait();
     volatile int* abort_flag = &s_abort;
 
     if (warp == 0) {
@@ -629,7 +685,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
             const auto hand_over = [&](int c, float* v) {
                 const int at_m = tile.m * kTileM + quad * 32, at_n = tile.n * BN + c * 32;
                 const int row0 = p.swap ? at_n : at_m, col0 = p.swap ? at_m : at_n;
-                if (p.copy_out) {
+                if (p.copy_out || (!p.swap && !p.residual)) {
                     send_block<T>(p, mine, bias, &sent, v, at_m, at_n, lane);
                     return;
                 }
@@ -765,67 +821,95 @@ struct DzArgs {
     int64_t rows, ld, ld_dz;
     int n, parts, act, db_fp32;
 };
-// A CTA goes down 128 bytes of columns; `parts` CTAs of a cluster share the rows and add their sums up in rank order.
-// WIDE: 16 bytes a thread; else (rows that do not start on 16-byte boundaries) value by value, a row per warp.
-template <typename T, bool WIDE>
+// 16 bytes from anywhere: the two aligned pieces that hold them, and their bits shifted into place.  Rows off 16-byte boundaries are read in
+// whole pieces too.
+template <bool SHIFT>
+struct Piece {
+    uint4 a, b;
+    __device__ __forceinline__ void load(const char* at)
+    {
+        const char* piece = SHIFT ? at - (reinterpret_cast<uintptr_t>(at) & 15) : at;
+        a = *reinterpret_cast<const uint4*>(piece);
+        if (SHIFT) b = *(reinterpret_cast<const uint4*>(piece) + 1);
+    }
+    __device__ __forceinline__ uint4 get(const char* at) const
+    {
+        if (!SHIFT) return a;
+        const uint32_t s = (uint32_t)(reinterpret_cast<uintptr_t>(at) & 15);
+        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = s & 8 ? w[i + 2] : w[i];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = s & 4 ? w[i + 1] : w[i];
+        const uint32_t bits = (s & 3) * 8;
+        return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+    }
+};
+
+// A CTA goes down 128 bytes of columns, 32 rows at a time; `parts` CTAs of a cluster share the rows and add their sums up in rank order.
+// The loads of U rows a thread are issued before the first is used.
+template <typename T, bool SHIFT>
 __global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ DzArgs p)
 {
-    constexpr int COLS = 128 / sizeof(T);
-    constexpr int V = WIDE ? 16 / (int)sizeof(T) : COLS / 32, STRIDE = WIDE ? 1 : 32, ROWS = WIDE ? 32 : 8;
+    constexpr int COLS = 128 / sizeof(T), V = Pack<T>::V, ROWS = 32, U = SHIFT ? 2 : 4;
     __shared__ float s_sum[8][COLS];
     __shared__ float s_total[COLS];
     const int part = (int)(blockIdx.x % (unsigned)p.parts);
     const int c0 = (int)(blockIdx.x / (unsigned)p.parts) * COLS;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int col = WIDE ? (threadIdx.x & 7) * V : lane;
-    const int r0 = WIDE ? threadIdx.x >> 3 : warp;
+    const int col = (threadIdx.x & 7) * V;
     float sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[j] = 0.f;
-    const bool whole = c0 + col + (V - 1) * STRIDE < p.n;
-#pragma unroll 4
-    for (int64_t r = (int64_t)part * ROWS + r0; r < p.rows; r += (int64_t)p.parts * ROWS) {
-        float g[V], z[V];
-        const T* dy = reinterpret_cast<const T*>(p.dy) + r * p.ld + c0 + col;
-        const T* zr = reinterpret_cast<const T*>(p.z) + r * p.ld + c0 + col;
-        if (WIDE && whole) {
-            if constexpr (WIDE) {
-                Pack<T>::unpack(*reinterpret_cast<const uint4*>(dy), g);
-                if (p.act != HPF_ACT_NONE) Pack<T>::unpack(*reinterpret_cast<const uint4*>(zr), z);
-            }
-        } else {
+    const T *dy = reinterpret_cast<const T*>(p.dy) + c0 + col, *z = reinterpret_cast<const T*>(p.z) + c0 + col;
+    T* dz = reinterpret_cast<T*>(p.dz) + c0 + col;
+    const bool act = p.act != HPF_ACT_NONE;
+    const int64_t step = (int64_t)p.parts * ROWS;
+    const int there = p.n - c0 - col;                        // columns from here on
+    pdl_launch_dependents();
+    pdl_wait();
+    for (int64_t r0 = (int64_t)part * ROWS + (threadIdx.x >> 3); r0 < p.rows; r0 += U * step) {
+        Piece<SHIFT> gp[U], zp[U];
+        bool whole[U];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const bool in = c0 + col + j * STRIDE < p.n;
-                g[j] = in ? Pack<T>::get(dy[j * STRIDE]) : 0.f;
-                z[j] = in && p.act != HPF_ACT_NONE ? Pack<T>::get(zr[j * STRIDE]) : 0.f;
+        for (int u = 0; u < U; ++u) {
+            // a shifted piece reaches up to 15 bytes to either side: never out of the first row's start nor of the last row's end
+            const int64_t r = r0 + u * step;
+            whole[u] = r < p.rows && there >= V;
+            if (SHIFT && ((r == 0 && c0 + col < V) || (r == p.rows - 1 && there < 2 * V))) whole[u] = false;
+            if (whole[u]) {
+                gp[u].load(reinterpret_cast<const char*>(dy + r * p.ld));
+                if (act) zp[u].load(reinterpret_cast<const char*>(z + r * p.ld));
             }
         }
-        if (p.act != HPF_ACT_NONE) apply_slope<V>(g, z, p.act);
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] += g[j];
-        if (p.dz) {
-            // dz is rounded to the operands' type: the tensor cores take it in that type only
-            T* out = reinterpret_cast<T*>(p.dz) + r * p.ld_dz + c0 + col;
-            if (WIDE && whole) {
-                if constexpr (WIDE) *reinterpret_cast<uint4*>(out) = Pack<T>::pack(g);
+        for (int u = 0; u < U; ++u) {
+            const int64_t r = r0 + u * step;
+            if (r >= p.rows) break;
+            float g[V], zv[V];
+            if (whole[u]) {
+                Pack<T>::unpack(gp[u].get(reinterpret_cast<const char*>(dy + r * p.ld)), g);
+                if (act) Pack<T>::unpack(zp[u].get(reinterpret_cast<const char*>(z + r * p.ld)), zv);
             } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (c0 + col + j * STRIDE < p.n) out[j * STRIDE] = Pack<T>::put(g[j]);
+                for (int j = 0; j < V; ++j) {
+                    g[j] = j < there ? Pack<T>::get(dy[r * p.ld + j]) : 0.f;
+                    zv[j] = j < there && act ? Pack<T>::get(z[r * p.ld + j]) : 0.f;
+                }
             }
+            if (act) apply_slope<V>(g, zv, p.act);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum[j] += g[j];
+            // dz is rounded to the operands' type: the tensor cores take it in that type only.  Its rows are whole numbers of 128 bytes long.
+            if (p.dz && there > 0) *reinterpret_cast<uint4*>(dz + r * p.ld_dz) = Pack<T>::pack(g);
         }
     }
     if (!p.db) return;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        if (WIDE) {
-            sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 8);
-            sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
-            if (lane < 8) s_sum[warp][col + j] = sum[j];
-        } else {
-            s_sum[warp][col + j * STRIDE] = sum[j];
-        }
+        sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 8);
+        sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
+        if (lane < 8) s_sum[warp][col + j] = sum[j];
     }
     __syncthreads();
     if (threadIdx.x < COLS) {
@@ -846,15 +930,18 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ 
 
 // Rows that a tensor copy cannot address (start or stride off 16 bytes), laid out again at a stride that it can.
 template <typename T>
-__global__ void __launch_bounds__(256) linear_repack_kernel(const T* __restrict__ in, T* __restrict__ out, int64_t rows, int n, int64_t ld, int64_t ld_out)
+__global__ void __launch_bounds__(256) linear_repack_kernel(const T* in, T* out, int64_t rows, int n, int64_t ld, int64_t ld_out)
 {
+    pdl_launch_dependents();
+    pdl_wait();
     for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (int64_t)gridDim.x * 8)
         for (int c = threadIdx.x & 31; c < n; c += 32) out[r * ld_out + c] = in[r * ld + c];
 }
 
 // ---- host side ----------------------------------------------------------------------------------------------------------
 size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-int64_t padded(int64_t n, int e) { return (n * e + 15) / 16 * 16 / e; }
+// rows of what is laid out in scratch: whole 128-byte lines (a row of a stage that straddles two took the copies 1.5 times as long)
+int64_t padded(int64_t n, int e) { return (n * e + 127) / 128 * 128 / e; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 int sm_count()
@@ -863,6 +950,28 @@ int sm_count()
     int n = 0;
     if (sms.get(&n, [](int dev, int* v) { return cudaDeviceGetAttribute(v, cudaDevAttrMultiProcessorCount, dev); }) != cudaSuccess) return 148;
     return n;
+}
+
+// Every kernel of this file is launched as a programmatic dependent: it may be scheduled while its predecessor in the stream drains, sets
+// itself up, and waits for the predecessor's results before its first access to global memory.  (A backward pass is three kernels, 2 us of
+// launch and set-up each otherwise.)
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kernel)(KArgs...), unsigned grid, int threads, size_t smem, int cluster, cudaStream_t st, const Args&... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 struct Operand {
@@ -909,18 +1018,8 @@ cudaError_t launch_gemm(GemmArgs& g, cudaStream_t st)
     cudaError_t e = attributes.get(&set, [&](int, bool* v) { *v = true; return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
     if (e != cudaSuccess) return e;
     const int tiles = g.tiles_m * g.tiles_n;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(g.split > 1 ? (unsigned)(tiles * g.split) : (unsigned)(tiles < sm_count() ? tiles : sm_count()));
-    cfg.blockDim = dim3(Shape<E, BN>::kThreads);
-    cfg.dynamicSmemBytes = kSmem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)g.split;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = g.split > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, g);
+    const unsigned grid = g.split > 1 ? (unsigned)(tiles * g.split) : (unsigned)(tiles < sm_count() ? tiles : sm_count());
+    return launch(kernel, grid, Shape<E, BN>::kThreads, kSmem, g.split, st, g);
 }
 
 // Clusters of 1, 2, 4 and 8 CTAs of this kernel's shape that the device holds at a time (one CTA per SM; a cluster stays within a GPC,
@@ -1040,31 +1139,20 @@ cudaError_t repack(const void* in, void* out, int64_t rows, int n, int64_t ld, i
 {
     const int64_t blocks = (rows + 7) / 8;
     const unsigned grid = (unsigned)(blocks < 8 * sm_count() ? blocks : 8 * sm_count());
-    if (e == 4) linear_repack_kernel<uint32_t><<<grid, 256, 0, st>>>(static_cast<const uint32_t*>(in), static_cast<uint32_t*>(out), rows, n, ld, ld_out);
-    else linear_repack_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t*>(in), static_cast<uint16_t*>(out), rows, n, ld, ld_out);
-    return cudaGetLastError();
+    if (e == 4) return launch(linear_repack_kernel<uint32_t>, grid, 256, 0, 1, st, static_cast<const uint32_t*>(in), static_cast<uint32_t*>(out), rows, n, ld, ld_out);
+    return launch(linear_repack_kernel<uint16_t>, grid, 256, 0, 1, st, static_cast<const uint16_t*>(in), static_cast<uint16_t*>(out), rows, n, ld, ld_out);
 }
 
 template <typename T>
 cudaError_t launch_dz(DzArgs& a, cudaStream_t st)
 {
     const int cols = 128 / sizeof(T);
-    const bool wide = aligned16(a.dy) && (a.ld * sizeof(T)) % 16 == 0 && (a.act == HPF_ACT_NONE || aligned16(a.z));
     // one CTA goes down up to 256 rows by itself: joining a cluster's sums takes longer than that
     const int64_t want = (a.rows + 255) / 256;
     a.parts = (int)(want > 8 ? 8 : want);
-    auto* kernel = wide ? linear_dz_kernel<T, true> : linear_dz_kernel<T, false>;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((a.n + cols - 1) / cols * a.parts));
-    cfg.blockDim = dim3(256);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)a.parts;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = a.parts > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, a);
+    const bool wide = aligned16(a.dy) && (a.ld * sizeof(T)) % 16 == 0 && (a.act == HPF_ACT_NONE || aligned16(a.z));
+    auto* kernel = wide ? linear_dz_kernel<T, false> : linear_dz_kernel<T, true>;
+    return launch(kernel, (unsigned)((a.n + cols - 1) / cols * a.parts), 256, 0, a.parts, st, a);
 }
 
 // ---- scratch: status word | dz | x laid out again | W laid out again ----------------------------------------------------

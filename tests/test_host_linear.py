@@ -54,11 +54,11 @@ def test_an_empty_batch_writes_nothing_forward():
 @pytest.mark.parametrize("dtype, e", [(torch.float32, 4), (torch.bfloat16, 2), (torch.float16, 2)])
 def test_scratch_holds_dz_and_what_a_copy_cannot_address(dtype, e):
     up = lambda v: (v + 255) // 256 * 256  # noqa: E731
-    pad = lambda n: (n * e + 15) // 16 * 16  # noqa: E731
+    pad = lambda n: (n * e + 127) // 128 * 128  # noqa: E731
     rows, n_in, n_out = 100, 64, 48
     assert hpf.linear_scratch_bytes(rows, n_in, n_out, n_in, n_out, dtype) == 256
-    assert hpf.linear_scratch_bytes(rows, n_in, n_out, n_in, n_out, dtype, hpf.ACT_GELU) == 256 + up(rows * n_out * e)
-    assert hpf.linear_scratch_bytes(rows, n_in, n_out, n_in + 1, n_out, dtype) == 256 + up(rows * n_in * e)
+    assert hpf.linear_scratch_bytes(rows, n_in, n_out, n_in, n_out, dtype, hpf.ACT_GELU) == 256 + up(rows * pad(n_out))
+    assert hpf.linear_scratch_bytes(rows, n_in, n_out, n_in + 1, n_out, dtype) == 256 + up(rows * pad(n_in))
     odd = 256 + up(rows * pad(51)) + up(rows * pad(33)) + up(51 * pad(33))
     assert hpf.linear_scratch_bytes(rows, 33, 51, 33, 51, dtype) == odd
     assert hpf.linear_scratch_bytes(rows, 32, 48, 32, 48, dtype, aligned=False) == 256 + up(rows * pad(48)) + up(rows * pad(32)) + up(48 * pad(32))
