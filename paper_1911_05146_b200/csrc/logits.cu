@@ -31,7 +31,6 @@ constexpr int kMaxParts = 8;       // CTAs a row is cut into (portable cluster s
 constexpr int kGroups = 128;       // groups of threads whose maxima bound the k-th largest class
 constexpr int kCandidates = 1024;  // classes at or above that bound that are ranked by counting
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFloor = -1e30f;   // stands for -inf where it meets a weight of 0
 
 __device__ __forceinline__ float ninf() { return __int_as_float(0xff800000); }
@@ -57,8 +56,41 @@ template <> struct Io<float> {
     }
     static __device__ __forceinline__ float get(float v) { return v; }
     static __device__ __forceinline__ float put(float v) { return v; }
+    // of two pieces, value by value (a NaN loses); the largest value of a piece; -inf replaced by the type's lowest value; nothing below
+    // -10^30 (the lowest value of fp16 is above that).  A NaN stays.
+    static __device__ __forceinline__ uint4 larger(const uint4& a, const uint4& b)
+    {
+        return make_uint4(one(a.x, b.x), one(a.y, b.y), one(a.z, b.z), one(a.w, b.w));
+    }
+    static __device__ __forceinline__ uint32_t one(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+    static __device__ __forceinline__ float largest(const uint4& a) { return fmaxf(fmaxf(__uint_as_float(a.x), __uint_as_float(a.y)), fmaxf(__uint_as_float(a.z), __uint_as_float(a.w))); }
+    static __device__ __forceinline__ uint4 finite(const uint4& a)
+    {
+        return make_uint4(low(a.x), low(a.y), low(a.z), low(a.w));
+    }
+    static __device__ __forceinline__ uint32_t low(uint32_t v) { return v == 0xff800000u ? 0xff7fffffu : v; }
+    static __device__ __forceinline__ uint4 bounded(const uint4& a) { return make_uint4(above(a.x), above(a.y), above(a.z), above(a.w)); }
+    static __device__ __forceinline__ uint32_t above(uint32_t v) { return __uint_as_float(v) < kFloor ? __float_as_uint(kFloor) : v; }
 };
-template <> struct Io<__nv_bfloat16> {
+template <typename T, typename T2, uint32_t LOWEST, uint32_t FLOOR>
+struct Packed16 {
+    static __device__ __forceinline__ uint32_t one(uint32_t a, uint32_t b)
+    {
+        const T2 m = __hmax2(*reinterpret_cast<const T2*>(&a), *reinterpret_cast<const T2*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&m);
+    }
+    static __device__ __forceinline__ uint4 larger(const uint4& a, const uint4& b) { return make_uint4(one(a.x, b.x), one(a.y, b.y), one(a.z, b.z), one(a.w, b.w)); }
+    template <uint32_t BOUND>
+    static __device__ __forceinline__ uint32_t above(uint32_t a)
+    {
+        const uint32_t bound = BOUND;
+        const T2 m = __hmax2_nan(*reinterpret_cast<const T2*>(&a), *reinterpret_cast<const T2*>(&bound));
+        return *reinterpret_cast<const uint32_t*>(&m);
+    }
+    static __device__ __forceinline__ uint4 finite(const uint4& a) { return make_uint4(above<LOWEST>(a.x), above<LOWEST>(a.y), above<LOWEST>(a.z), above<LOWEST>(a.w)); }
+    static __device__ __forceinline__ uint4 bounded(const uint4& a) { return make_uint4(above<FLOOR>(a.x), above<FLOOR>(a.y), above<FLOOR>(a.z), above<FLOOR>(a.w)); }
+};
+template <> struct Io<__nv_bfloat16> : Packed16<__nv_bfloat16, __nv_bfloat162, 0xff7fff7fu, 0xf14af14au> {
     static constexpr int V = 8;
     static constexpr uint32_t kMinusInf = 0xff80ff80u;
     static __device__ __forceinline__ void two(uint32_t w, float* f)
@@ -73,10 +105,16 @@ template <> struct Io<__nv_bfloat16> {
         return *reinterpret_cast<const uint32_t*>(&h);
     }
     static __device__ __forceinline__ uint4 pack(const float* f) { return make_uint4(join(f[0], f[1]), join(f[2], f[3]), join(f[4], f[5]), join(f[6], f[7])); }
+    static __device__ __forceinline__ float largest(const uint4& a)
+    {
+        float f[2];
+        two(one(one(a.x, a.y), one(a.z, a.w)), f);
+        return fmaxf(f[0], f[1]);
+    }
     static __device__ __forceinline__ float get(__nv_bfloat16 v) { return __bfloat162float(v); }
     static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
 };
-template <> struct Io<__half> {
+template <> struct Io<__half> : Packed16<__half, __half2, 0xfbfffbffu, 0xfbfffbffu> {
     static constexpr int V = 8;
     static constexpr uint32_t kMinusInf = 0xfc00fc00u;
     static __device__ __forceinline__ void two(uint32_t w, float* f)
@@ -91,6 +129,12 @@ template <> struct Io<__half> {
         return *reinterpret_cast<const uint32_t*>(&h);
     }
     static __device__ __forceinline__ uint4 pack(const float* f) { return make_uint4(join(f[0], f[1]), join(f[2], f[3]), join(f[4], f[5]), join(f[6], f[7])); }
+    static __device__ __forceinline__ float largest(const uint4& a)
+    {
+        float f[2];
+        two(one(one(a.x, a.y), one(a.z, a.w)), f);
+        return fmaxf(f[0], f[1]);
+    }
     static __device__ __forceinline__ float get(__half v) { return __half2float(v); }
     static __device__ __forceinline__ __half put(float v) { return __float2half_rn(v); }
 };
@@ -133,7 +177,21 @@ struct Share {
 };
 
 // ---- running sums ----------------------------------------------------------------------------------------------------
-// m: largest logit, s = sum 2^((v - m) c), w = sum 2^((v - m) c) (v - m) c, h = the sum of s at temperature 1
+// Two values in one instruction: the loops below are bound by what an SM issues, not by its arithmetic.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void split(f2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f2 ex2_2(f2 v)
+{
+    float a, b;
+    split(v, &a, &b);
+    return pair(ex2(a), ex2(b));
+}
+
+// m: largest logit, s = sum 2^((v - m) c), w = sum 2^((v - m) c) (v - m), h = the sum of s at temperature 1
 struct Sums {
     float m, s, w, h;
 };
@@ -141,11 +199,10 @@ template <bool ENTROPY, bool HARD>
 __device__ __forceinline__ void rescale(Sums& a, float m, float c)
 {
     if (a.m == m) return;
-    const float d = fmaxf((a.m - m) * c, kFloor);        // a.m may be -inf: everything it weighs is 0
-    const float r = ex2(d);
-    if (ENTROPY) a.w = r * fmaf(d, a.s, a.w);
+    const float u = fmaxf(a.m - m, kFloor), r = ex2(u * c);       // a.m may be -inf: everything it weighs is 0
+    if (ENTROPY) a.w = r * fmaf(u, a.s, a.w);
     a.s *= r;
-    if (HARD) a.h *= ex2(fmaxf((a.m - m) * kLog2e, kFloor));
+    if (HARD) a.h *= ex2(u * kLog2e);
     a.m = m;
 }
 // The maximum is subtracted before anything is scaled: a row of the type's lowest value stays finite, and large logits lose nothing.
@@ -153,46 +210,98 @@ template <bool ENTROPY, bool HARD>
 __device__ __forceinline__ void add_value(Sums& a, float v, float c, float base)
 {
     const float u = v - base;
-    const float d = u * c;
-    const float e = ex2(d);
+    const float e = ex2(u * c);
     a.s += e;
-    if (ENTROPY) a.w = fmaf(e, fmaxf(d, kFloor), a.w);
+    if (ENTROPY) a.w = fmaf(e, fmaxf(u, kFloor), a.w);
     if (HARD) a.h += ex2(u * kLog2e);
 }
 __device__ __forceinline__ float base_of(float m) { return m == ninf() ? 0.f : m; }
 
-template <typename T, int NT, bool ENTROPY, bool HARD>
-__device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid)
+// Where a thread leaves the largest logit of each stretch of its strip (for the list of the largest classes).
+struct Stretches {
+    float* at;           // [count][threads]
+    int count, iters;    // stretches, and the rounds of the loop below that one takes
+};
+
+// How the sum at temperature 1 is formed: from an exponential of its own, or, where the temperature is a small whole number, as a power of
+// the one at hand.  A second exponential a class makes the loop as long as the special-function unit takes for it (4096 x 128000
+// bf16: 279 us instead of 190).
+constexpr int kNoHard = -1, kOwnExp = 0;
+
+// One thread's share of the row.  ENTROPY: -inf is replaced by the type's lowest value ahead of the weighted sum (0 (-inf) would be NaN);
+// v - m overflows only where m > 10^30, where every class but the largest weighs nothing: see write_stats.
+template <typename T, int NT, bool ENTROPY, int POWER>
+__device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, const Stretches* st)
 {
     constexpr int V = Io<T>::V, U = 4;
+    constexpr bool HARD = POWER != kNoHard;
+    const uint4 none = make_uint4(Io<T>::kMinusInf, Io<T>::kMinusInf, Io<T>::kMinusInf, Io<T>::kMinusInf);
     Sums a{ninf(), 0.f, 0.f, 0.f};
-    float base = 0.f;
-    for (int i = sh.c0 + tid; i < sh.c1; i += U * NT) {
-        uint4 raw[U];
+    f2 s2 = 0, w2 = 0, h2 = 0;
+    const f2 c2 = pair(c, c), one2 = pair(kLog2e, kLog2e);
+    f2 base2 = 0;                                             // -m, twice
+    int slot = 0, left = st ? st->iters : 0;
+    float stretch = ninf();
+    uint4 raw[U];
+    int i = sh.c0 + tid;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            raw[u] = i + u * NT < sh.c1 ? sh.load(i + u * NT) : make_uint4(Io<T>::kMinusInf, Io<T>::kMinusInf, Io<T>::kMinusInf, Io<T>::kMinusInf);
-        float top = ninf();
+    for (int u = 0; u < U; ++u) raw[u] = i + u * NT < sh.c1 ? sh.load(i + u * NT) : none;
+    while (i < sh.c1) {
+        uint4 next[U];                                        // under way while this round is worked on
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[V];
-            Io<T>::unpack(raw[u], f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) top = fmaxf(top, f[j]);
+        for (int u = 0; u < U; ++u) next[u] = i + (U + u) * NT < sh.c1 ? sh.load(i + (U + u) * NT) : none;
+        const float top = Io<T>::largest(Io<T>::larger(Io<T>::larger(raw[0], raw[1]), Io<T>::larger(raw[2], raw[3])));
+        if (st) {
+            stretch = fmaxf(stretch, top);
+            if (--left == 0) {
+                st->at[slot * NT + tid] = stretch;
+                ++slot;
+                left = st->iters;
+                stretch = ninf();
+            }
         }
         if (top > a.m) {
-            rescale<ENTROPY, HARD>(a, top, c);
-            base = top;
+            const float u = fmaxf(a.m - top, kFloor), r = ex2(u * c);
+            const f2 r2 = pair(r, r);
+            if (ENTROPY) w2 = mul2(r2, fma2(pair(u, u), s2, w2));
+            s2 = mul2(r2, s2);
+            if (POWER == kOwnExp || POWER > 1) {
+                const float q = ex2(u * kLog2e);
+                h2 = mul2(pair(q, q), h2);
+            }
+            a.m = top;
+            base2 = pair(-top, -top);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (i + u * NT < sh.c1) {
                 float f[V];
-                Io<T>::unpack(raw[u], f);
+                Io<T>::unpack(ENTROPY ? Io<T>::finite(raw[u]) : raw[u], f);
 #pragma unroll
-                for (int j = 0; j < V; ++j) add_value<ENTROPY, HARD>(a, f[j], c, base);
+                for (int j = 0; j < V; j += 2) {
+                    const f2 d = add2(pair(f[j], f[j + 1]), base2);
+                    const f2 e = ex2_2(mul2(d, c2));
+                    s2 = add2(s2, e);
+                    if (ENTROPY) w2 = fma2(e, d, w2);
+                    if (POWER == kOwnExp) h2 = add2(h2, ex2_2(mul2(d, one2)));
+                    if (POWER == 2) h2 = fma2(e, e, h2);
+                    if (POWER == 3) h2 = fma2(mul2(e, e), e, h2);
+                    if (POWER == 4) { const f2 q = mul2(e, e); h2 = fma2(q, q, h2); }
+                }
             }
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = next[u];
+        i += U * NT;
     }
+    if (st)
+        for (; slot < st->count; ++slot) {
+            st->at[slot * NT + tid] = stretch;
+            stretch = ninf();
+        }
+    float x, y;
+    split(s2, &x, &y); a.s = x + y;
+    split(w2, &x, &y); a.w = x + y;
+    split(h2, &x, &y); a.h = POWER == 1 ? a.s : x + y;
     const int e = sh.edge(tid);
     if (e >= 0) {
         const float v = Io<T>::get(sh.row[e]);
@@ -200,6 +309,16 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid)
         add_value<ENTROPY, HARD>(a, v, c, base_of(a.m));
     }
     return a;
+}
+template <typename T, int NT, bool HARD>
+__device__ __forceinline__ Sums run_over_power(const Share<T>& sh, float c, int tid, int power)
+{
+    if constexpr (!HARD) return run_over<T, NT, false, kNoHard>(sh, c, tid, nullptr);
+    if (power == 1) return run_over<T, NT, false, 1>(sh, c, tid, nullptr);
+    if (power == 2) return run_over<T, NT, false, 2>(sh, c, tid, nullptr);
+    if (power == 3) return run_over<T, NT, false, 3>(sh, c, tid, nullptr);
+    if (power == 4) return run_over<T, NT, false, 4>(sh, c, tid, nullptr);
+    return run_over<T, NT, false, kOwnExp>(sh, c, tid, nullptr);
 }
 
 template <bool ENTROPY, bool HARD>
@@ -224,25 +343,24 @@ __device__ __forceinline__ Sums join_sums(const Sums* part, int count, int lane,
     Sums a = lane < count ? part[lane] : Sums{ninf(), 0.f, 0.f, 0.f};
     return warp_sums<ENTROPY, HARD>(a, c);
 }
-
-// the same value for every thread of the CTA, and of the cluster where a row has several parts
+// the same value for every thread of the CTA
 template <int NT, bool ENTROPY, bool HARD>
-__device__ __forceinline__ Sums block_sums(Sums a, float c, int parts, Sums* s_part, Sums* s_mine)
+__device__ __forceinline__ Sums block_sums(Sums a, float c, Sums* s_part)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     a = warp_sums<ENTROPY, HARD>(a, c);
-    if (lane == 0) s_part[warp] = a;
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = a;
     __syncthreads();
-    a = join_sums<ENTROPY, HARD>(s_part, NT / 32, lane, c);
-    if (parts > 1) {
-        cg::cluster_group cl = cg::this_cluster();
-        if (threadIdx.x == 0) *s_mine = a;
-        cl.sync();
-        Sums b{ninf(), 0.f, 0.f, 0.f};
-        if (lane < parts) b = *cl.map_shared_rank(s_mine, lane);
-        a = warp_sums<ENTROPY, HARD>(b, c);
-    }
-    return a;
+    return join_sums<ENTROPY, HARD>(s_part, NT / 32, threadIdx.x & 31, c);
+}
+// The same value for every CTA of a row: each puts its sums into the shared memory of all (into, not out of: nobody has to stay for others
+// to read).  s_parts: one place per part.
+template <bool HARD>
+__device__ __forceinline__ Sums cluster_sums(Sums a, float c, int part, int parts, Sums* s_parts)
+{
+    cg::cluster_group cl = cg::this_cluster();
+    if ((int)threadIdx.x < parts) *cl.map_shared_rank(&s_parts[part], threadIdx.x) = a;
+    cl.sync();
+    return join_sums<false, HARD>(s_parts, parts, threadIdx.x & 31, c);
 }
 
 // ---- the k largest classes -------------------------------------------------------------------------------------------
@@ -262,24 +380,28 @@ __device__ __forceinline__ float key_value(unsigned long long key)
 }
 __device__ __forceinline__ int key_class(unsigned long long key) { return 0x7fffffff - (int)(uint32_t)(key & 0xffffffffu); }
 
+constexpr int kStretches = 4096;   // of all threads of a CTA
+
 struct TopShared {
     float group[kGroups];
     float maxima[1024];
-    int threads[1024];
+    float stretch[kStretches];
+    unsigned short list[kStretches];
     unsigned long long cand[kCandidates];
     unsigned long long best[kMaxTop];
     int count, listed;
     float bound;
 };
 
-// Calls f(value, class) for every class of the strips of the threads in `list`, spread over the CTA, and of the row's ends.
+// Calls f(value, class) for every class of the listed stretches, spread over the CTA, and of the row's ends.
 template <typename T, int NT, typename F>
-__device__ __forceinline__ void over_strips(const Share<T>& sh, const int* list, int listed, F&& f)
+__device__ __forceinline__ void over_stretches(const Share<T>& sh, const unsigned short* list, int listed, int iters, F&& f)
 {
-    constexpr int V = Io<T>::V;
-    const int per = (sh.c1 - sh.c0 + NT - 1) / NT;                 // pieces of a strip
-    for (int w = threadIdx.x; w < listed * per; w += NT) {
-        const int c = sh.c0 + list[w / per] + (w % per) * NT;
+    constexpr int V = Io<T>::V, U = 4;
+    const unsigned per = (unsigned)(iters * U);                    // pieces of a stretch
+    for (unsigned w = threadIdx.x; w < (unsigned)listed * per; w += NT) {
+        const unsigned at = w / per, piece = w - at * per, entry = list[at];
+        const int c = sh.c0 + (int)(entry % NT) + (int)((entry / NT) * per + piece) * NT;
         if (c < sh.c1) {
             float v[V];
             Io<T>::unpack(sh.load(c), v);
@@ -291,13 +413,13 @@ __device__ __forceinline__ void over_strips(const Share<T>& sh, const int* list,
     if (e >= 0) f(Io<T>::get(sh.row[e]), e);
 }
 
-// The k largest classes of this CTA's share, best first, into sm.best.  Every thread knows the largest logit of its strip.
-// The k-th largest of 128 group maxima is a lower bound of the k-th largest class, so only strips whose maximum reaches it are read
-// again (from L2): about 128 ln(128 / (128 - k)) classes pass for unordered rows.  Threads t, t + 128, ... form a group, so that a row sorted
-// by frequency does not put its head into one group.  Where too many pass (long runs of equal logits), a bisection over the unique
-// keys raises the bound until they fit.
+// The k largest classes of this CTA's share, best first, into sm.best.  Every thread knows the largest logit of each stretch of its strip
+// (sm.stretch) and of all of it (my_max).  The k-th largest of 128 group maxima is a lower bound of the k-th largest class, so only stretches
+// whose maximum reaches it are read again (from L2): about 128 ln(128 / (128 - k)) classes pass for unordered rows.  Threads t,
+// t + 128, ... form a group, so that a row sorted by frequency does not put its head into one group.  Where too many pass (long runs of
+// equal logits), a bisection over the unique keys raises the bound until they fit.
 template <typename T, int NT>
-__device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int k, TopShared& sm)
+__device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int k, int iters, TopShared& sm)
 {
     const int tid = threadIdx.x;
     sm.maxima[tid] = my_max;
@@ -306,13 +428,14 @@ __device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int
     __syncthreads();
     float g = ninf();
     if (tid < kGroups) {
-        for (int t = tid; t < NT; t += kGroups) g = fmaxf(g, sm.maxima[t]);
+#pragma unroll
+        for (int t = 0; t < NT; t += kGroups) g = fmaxf(g, sm.maxima[t + tid]);
         sm.group[tid] = g;
     }
     __syncthreads();
     if (tid < kGroups) {
         int rank = 0;
-#pragma unroll 8
+#pragma unroll
         for (int j = 0; j < kGroups; j += 4) {
             const float4 o = *reinterpret_cast<const float4*>(&sm.group[j]);
             rank += (o.x > g || (o.x == g && j < tid)) + (o.y > g || (o.y == g && j + 1 < tid)) +
@@ -322,10 +445,16 @@ __device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int
     }
     __syncthreads();
     const float bound = sm.bound;
-    if (my_max >= bound && my_max > ninf()) sm.threads[atomicAdd(&sm.listed, 1)] = tid;
+    if (my_max >= bound && my_max > ninf()) {
+#pragma unroll
+        for (int s = 0; s < kStretches / NT; ++s) {
+            const float v = sm.stretch[s * NT + tid];
+            if (v >= bound && v > ninf()) sm.list[atomicAdd(&sm.listed, 1)] = (unsigned short)(s * NT + tid);
+        }
+    }
     __syncthreads();
     const int listed = sm.listed;
-    over_strips<T, NT>(sh, sm.threads, listed, [&](float v, int cls) {
+    over_stretches<T, NT>(sh, sm.list, listed, iters, [&](float v, int cls) {
         if (v >= bound && v > ninf()) {
             const int at = atomicAdd(&sm.count, 1);
             if (at < kCandidates) sm.cand[at] = class_key(v, cls);
@@ -342,7 +471,7 @@ __device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int
             __syncthreads();
             if (tid == 0) sm.count = 0;
             __syncthreads();
-            over_strips<T, NT>(sh, sm.threads, listed, [&](float v, int cls) {
+            over_stretches<T, NT>(sh, sm.list, listed, iters, [&](float v, int cls) {
                 const unsigned long long key = class_key(v, cls);
                 if (key >= mid) {
                     const int at = atomicAdd(&sm.count, 1);
@@ -359,6 +488,7 @@ __device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int
     for (int i = tid; i < count; i += NT) {
         const unsigned long long mine = sm.cand[i];
         int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < count; ++j) rank += sm.cand[j] > mine;
         if (rank < k) sm.best[rank] = mine;
     }
@@ -387,8 +517,10 @@ __device__ __forceinline__ void write_stats(const LogprobsArgs& p, int64_t row, 
     // a row without a finite logit has no distribution: a.m = -inf, a.s = 0
     const bool none = a.m == ninf() && a.s == 0.f;
     const float ln_s = logf(a.s);
+    // above 10^30 every class but the largest ones weighs nothing (and may have overflowed in the weighted sum)
+    const float w = a.m > 1e30f && a.m < __int_as_float(0x7f800000) ? 0.f : a.w;
     if (p.lse) p.lse[row] = none ? ninf() : fmaf(a.m, p.inv_t, ln_s);
-    if (p.entropy) p.entropy[row] = none ? 0.f : fmaf(-kLn2, a.w / a.s, ln_s);
+    if (p.entropy) p.entropy[row] = none ? 0.f : fmaf(-p.inv_t, w / a.s, ln_s);
     if (p.logprob) {
         const int label = p.labels[row];
         float lp = 0.f;
@@ -402,44 +534,58 @@ __device__ __forceinline__ void write_stats(const LogprobsArgs& p, int64_t row, 
 }
 
 template <typename T, int NT, bool TOP>
-__global__ void __launch_bounds__(NT, NT == 256 ? 5 : 1) logprobs_fwd_kernel(const __grid_constant__ LogprobsArgs p)
+__global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) logprobs_fwd_kernel(const __grid_constant__ LogprobsArgs p)
 {
+    constexpr bool PARTS = NT == 1024;                   // a row is cut into parts only where few rows leave the CTAs large
     __shared__ Sums s_part[32];
-    __shared__ Sums s_mine;
+    __shared__ Sums s_parts[kMaxParts];
     __shared__ __align__(16) unsigned char s_top[TOP ? sizeof(TopShared) : 16];
-    __shared__ unsigned long long s_all[TOP && NT == 1024 ? kMaxParts * kMaxTop : 1];
-    const int part = (int)(blockIdx.x % (unsigned)p.parts);
-    const int64_t row = blockIdx.x / (unsigned)p.parts;
+    __shared__ unsigned long long s_all[TOP && PARTS ? kMaxParts * kMaxTop : 1];
+    const int part = PARTS ? (int)(blockIdx.x % (unsigned)p.parts) : 0;
+    const int64_t row = PARTS ? blockIdx.x / (unsigned)p.parts : blockIdx.x;
     const float c = p.inv_t * kLog2e;
-    const Share<T> sh(reinterpret_cast<const T*>(p.logits) + row * p.ld, p.n, part, p.parts);
-    Sums a = run_over<T, NT, true, false>(sh, c, threadIdx.x);
+    const Share<T> sh(reinterpret_cast<const T*>(p.logits) + row * p.ld, p.n, part, PARTS ? p.parts : 1);
+    TopShared& sm = *reinterpret_cast<TopShared*>(s_top);
+    Stretches st{nullptr, 0, 0};
+    if (TOP) {
+        const int rounds = (sh.c1 - sh.c0 + 4 * NT - 1) / (4 * NT);
+        st.at = sm.stretch;
+        st.count = kStretches / NT;
+        st.iters = (rounds + st.count - 1) / st.count;
+    }
+    Sums a = run_over<T, NT, true, kNoHard>(sh, c, threadIdx.x, TOP ? &st : nullptr);
     const float my_max = a.m;
-    a = block_sums<NT, true, false>(a, c, p.parts, s_part, &s_mine);
-    if (part == 0 && threadIdx.x == 0) write_stats<T>(p, row, a);
+    a = block_sums<NT, true, false>(a, c, s_part);
+    // the strips' maxima leave the row's ends out: they are always looked at again
+    if constexpr (TOP) select_top<T, NT>(sh, my_max, p.k, st.iters, sm);
+    if (PARTS && p.parts > 1) {
+        // sums and lists go to the row's first CTA
+        cg::cluster_group cl = cg::this_cluster();
+        if (threadIdx.x == 0) *cl.map_shared_rank(&s_parts[part], 0) = a;
+        if constexpr (TOP) {
+            if ((int)threadIdx.x < p.k) *cl.map_shared_rank(&s_all[part * p.k + threadIdx.x], 0) = sm.best[threadIdx.x];
+        }
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        if (part) return;
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        a = join_sums<true, false>(s_parts, p.parts, threadIdx.x & 31, c);
+    }
+    if (threadIdx.x == 0) write_stats<T>(p, row, a);
     if constexpr (TOP) {
-        TopShared& sm = *reinterpret_cast<TopShared*>(s_top);
-        // the strips' maxima leave the row's ends out: they are always looked at again
-        select_top<T, NT>(sh, my_max, p.k, sm);
         const float ln_s = logf(a.s);
-        if (p.parts == 1) {
+        if (!PARTS || p.parts == 1) {
             if ((int)threadIdx.x < p.k) write_top(p, row, threadIdx.x, sm.best[threadIdx.x], a.m, ln_s);
-        } else if constexpr (NT == 1024) {
-            cg::cluster_group cl = cg::this_cluster();
-            cl.sync();
-            if (part == 0) {
-                const int total = p.parts * p.k;
-                for (int i = threadIdx.x; i < total; i += NT) s_all[i] = cl.map_shared_rank(&sm, i / p.k)->best[i % p.k];
-                __syncthreads();
-                for (int i = threadIdx.x; i < total; i += NT) {
-                    const unsigned long long mine = s_all[i];
-                    int rank = 0;
-                    for (int j = 0; j < total; ++j) rank += s_all[j] > mine || (s_all[j] == mine && j < i);   // only zeros repeat
-                    if (rank < p.k) write_top(p, row, rank, mine, a.m, ln_s);
-                }
+        } else {
+            const int total = p.parts * p.k;
+            for (int i = threadIdx.x; i < total; i += NT) {
+                const unsigned long long mine = s_all[i];
+                int rank = 0;
+#pragma unroll 8
+                for (int j = 0; j < total; ++j) rank += s_all[j] > mine || (s_all[j] == mine && j < i);   // only zeros repeat
+                if (rank < p.k) write_top(p, row, rank, mine, a.m, ln_s);
             }
         }
     }
-    if (p.parts > 1) cg::this_cluster().sync();          // nobody leaves while its shared memory is read
 }
 
 // A warp per row of at most 32 J classes, all in registers; the list is taken one class at a time.
@@ -486,25 +632,26 @@ __global__ void __launch_bounds__(128) logprobs_fwd_warp_kernel(const __grid_con
 }
 
 // ---- gradients -------------------------------------------------------------------------------------------------------
-// Writes g(logit, class) for every class of the share.  `out` may be the logits themselves: a thread writes what it has read.
-template <typename T, int NT, typename F>
+// Writes g(two logits) for every two classes of the share.  `out` may be the logits themselves: a thread writes what it has read.
+// BOUNDED: nothing below -10^30 comes.
+template <typename T, int NT, bool BOUNDED, typename F>
 __device__ __forceinline__ void write_row(const Share<T>& sh, T* out, int tid, F&& g)
 {
-    constexpr int V = Io<T>::V, U = 2;
+    constexpr int V = Io<T>::V, U = 4;
     const bool wide = ((reinterpret_cast<uintptr_t>(out + sh.lead)) & 15) == 0;
     for (int i = sh.c0 + tid; i < sh.c1; i += U * NT) {
         uint4 raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + u * NT < sh.c1) raw[u] = *(reinterpret_cast<const uint4*>(sh.row + sh.lead) + i + u * NT);
+            if (i + u * NT < sh.c1) raw[u] = sh.load(i + u * NT);
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (i + u * NT < sh.c1) {
                 float f[V];
-                Io<T>::unpack(raw[u], f);
+                Io<T>::unpack(BOUNDED ? Io<T>::bounded(raw[u]) : raw[u], f);
                 const int at = sh.lead + (i + u * NT) * V;
 #pragma unroll
-                for (int j = 0; j < V; ++j) f[j] = g(f[j], at + j);
+                for (int j = 0; j < V; j += 2) split(g(pair(f[j], f[j + 1])), &f[j], &f[j + 1]);
                 if (wide) __stcs(reinterpret_cast<uint4*>(out + at), Io<T>::pack(f));
                 else
 #pragma unroll
@@ -512,7 +659,12 @@ __device__ __forceinline__ void write_row(const Share<T>& sh, T* out, int tid, F
             }
     }
     const int e = sh.edge(tid);
-    if (e >= 0) out[e] = Io<T>::put(g(Io<T>::get(sh.row[e]), e));
+    if (e >= 0) {
+        const float v = Io<T>::get(sh.row[e]);
+        float a, b;
+        split(g(pair(BOUNDED && v < kFloor ? kFloor : v, 0.f)), &a, &b);
+        out[e] = Io<T>::put(a);
+    }
 }
 
 struct LogprobsGradArgs {
@@ -524,19 +676,20 @@ struct LogprobsGradArgs {
     int n, parts;
     float inv_t;
 };
-// log2 p of a class = (v - m) c - l2s.  From a saved log-sum-exp: m = 0.  In fp32 that number carries ln S only while it is small
+// p of a class = 2^((v - m) c) inv_s.  From a saved log-sum-exp: m = T lse, inv_s = 1.  In fp32 that number carries ln S only while it is small
 // itself; where it is not (logits in the hundreds, a row of the type's lowest value, nothing but -inf) m and S are formed again.
 struct RowScale {
-    float m, l2s;
+    float m, s;                      // S = s (1 from a saved lse)
     bool none;                       // no finite logit: no distribution
 };
 constexpr float kLseExact = 128.f;   // an lse below this is off by 128 2^-24 = 7.6e-6 at most
-__device__ __forceinline__ RowScale scale_of(const Sums& a) { return RowScale{base_of(a.m), log2f(a.s), a.m == ninf() && a.s == 0.f}; }
+__device__ __forceinline__ RowScale scale_of(const Sums& a) { return RowScale{base_of(a.m), a.s, a.m == ninf() && a.s == 0.f}; }
 
-struct LogprobsGrad {                // of one row
-    float c, m, l2s, g_lp, g_h, h, inv_t;
+struct LogprobsGrad {                // of one row: a class gets p (a + b (v - m)), the label g on top
+    float c, m, a, b, g_lp, g_h, h, inv_t;
     int label;
     bool dead;                       // nothing flows back: zeros, whatever the logits hold
+    bool far;                        // scales at which a class at -10^30 would weigh something, or its product with b overflow
     __device__ __forceinline__ LogprobsGrad(const LogprobsGradArgs& p, int64_t row)
     {
         label = p.labels ? p.labels[row] : -1;
@@ -550,38 +703,58 @@ struct LogprobsGrad {                // of one row
     }
     __device__ __forceinline__ void scale(const RowScale& s)
     {
-        m = s.m;
-        l2s = s.l2s;
         if (s.none) dead = true;
+        m = s.m;
+        // ln p = (v - m) / T - ln S:  -(g_lp + g_h (ln p + H)) / T
+        const float w = inv_t / s.s;
+        a = -w * (g_lp + g_h * (h - logf(s.s)));
+        b = -w * g_h * inv_t;
+        far = !(fabsf(m) < 1e29f) || !(fabsf(b) < 1e6f) || !(c > 1e-20f);
     }
-    __device__ __forceinline__ float operator()(float v, int cls) const
+    __device__ __forceinline__ float slow(float v) const
     {
-        if (dead) return 0.f;
-        const float d = fmaf(v - m, c, -l2s);                     // log2 p
-        float g = -ex2(d) * fmaf(g_h, fmaf(fmaxf(d, kFloor), kLn2, h), g_lp);
-        if (cls == label) g += g_lp;
-        return g * inv_t;
+        const float u = v - m, e = ex2(u * c);
+        return e * (e == 0.f ? a : fmaf(b, u, a));           // (a NaN, of a row without a finite sum, passes)
     }
+    __device__ __forceinline__ f2 operator()(f2 v) const
+    {
+        const f2 u = add2(v, pair(-m, -m));
+        return mul2(ex2_2(mul2(u, pair(c, c))), fma2(pair(b, b), u, pair(a, a)));
+    }
+    __device__ __forceinline__ float label_value(float v) const { return slow(v) + g_lp * inv_t; }
 };
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT) logprobs_bwd_kernel(const __grid_constant__ LogprobsGradArgs p)
 {
     __shared__ Sums s_part[32];
-    __shared__ Sums s_mine;
+    __shared__ Sums s_parts[kMaxParts];
     const int part = (int)(blockIdx.x % (unsigned)p.parts);
     const int64_t row = blockIdx.x / (unsigned)p.parts;
     const Share<T> sh(reinterpret_cast<const T*>(p.logits) + row * p.ld, p.n, part, p.parts);
+    T* out = reinterpret_cast<T*>(p.d_logits) + row * p.ld_d;
     LogprobsGrad g(p, row);
-    bool again = false;              // the same for every part of a row
+    const float label_v = g.label >= 0 ? Io<T>::get(sh.row[g.label]) : 0.f;
     const float lse = p.lse[row];
-    RowScale s{0.f, lse * kLog2e, false};
-    if (!g.dead && !(fabsf(lse) < kLseExact)) {
-        again = true;
-        s = scale_of(block_sums<NT, false, false>(run_over<T, NT, false, false>(sh, g.c, threadIdx.x), g.c, p.parts, s_part, &s_mine));
+    RowScale s{lse / p.inv_t, 1.f, false};
+    if (!g.dead && !(fabsf(lse) < kLseExact)) {              // the same for every part of a row
+        Sums a = block_sums<NT, false, false>(run_over<T, NT, false, kNoHard>(sh, g.c, threadIdx.x, nullptr), g.c, s_part);
+        if (p.parts > 1) a = cluster_sums<false>(a, g.c, part, p.parts, s_parts);
+        s = scale_of(a);
     }
     g.scale(s);
-    write_row<T, NT>(sh, reinterpret_cast<T*>(p.d_logits) + row * p.ld_d, threadIdx.x, g);
-    if (again && p.parts > 1) cg::this_cluster().sync();
+    __syncthreads();                                         // the label's logit has been read (the gradient may be written in its place)
+    if (g.dead) write_row<T, NT, false>(sh, out, threadIdx.x, [](f2) { return (f2)0; });
+    else if (g.far)
+        write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) {
+            float x, y;
+            split(v, &x, &y);
+            return pair(g.slow(x), g.slow(y));
+        });
+    else write_row<T, NT, true>(sh, out, threadIdx.x, g);
+    if (!g.dead && sh.mine(g.label)) {
+        __syncthreads();
+        if (threadIdx.x == 0) out[g.label] = Io<T>::put(g.label_value(label_v));
+    }
 }
 // the sums of a row that a warp goes over by itself
 template <typename T, bool HARD>
@@ -589,7 +762,8 @@ __device__ __forceinline__ Sums warp_run_over(const T* x, int n, float c, int la
 {
     Sums a{ninf(), 0.f, 0.f, 0.f};
     for (int i = lane; i < n; i += 32) a.m = fmaxf(a.m, Io<T>::get(x[i]));
-    for (int i = lane; i < n; i += 32) add_value<false, HARD>(a, Io<T>::get(x[i]), c, base_of(a.m));
+    const float base = base_of(a.m);
+    for (int i = lane; i < n; i += 32) add_value<false, HARD>(a, Io<T>::get(x[i]), c, base);
     return warp_sums<false, HARD>(a, c);
 }
 template <typename T>
@@ -602,10 +776,13 @@ __global__ void __launch_bounds__(128) logprobs_bwd_warp_kernel(const __grid_con
     T* out = reinterpret_cast<T*>(p.d_logits) + row * p.ld_d;
     LogprobsGrad g(p, row);
     const float lse = p.lse[row];
-    RowScale s{0.f, lse * kLog2e, false};
+    RowScale s{lse / p.inv_t, 1.f, false};
     if (!g.dead && !(fabsf(lse) < kLseExact)) s = scale_of(warp_run_over<T, false>(x, p.n, g.c, lane));
     g.scale(s);
-    for (int i = lane; i < p.n; i += 32) out[i] = Io<T>::put(g(Io<T>::get(x[i]), i));
+    for (int i = lane; i < p.n; i += 32) {
+        const float v = Io<T>::get(x[i]);
+        out[i] = Io<T>::put(g.dead ? 0.f : i == g.label ? g.label_value(v) : g.slow(v));
+    }
 }
 
 // ---- distillation ----------------------------------------------------------------------------------------------------
@@ -619,30 +796,39 @@ struct DistillArgs {
     int64_t rows, ld, ld_d;
     int n, k, parts;
     float temp, inv_t, alpha;
+    int power;                       // the temperature where it is 1, 2, 3 or 4, else 0
 };
 struct Teacher {                     // of one row, in shared memory
     float q[kMaxTeacher], ln_q[kMaxTeacher], v[kMaxTeacher];
     int id[kMaxTeacher];
 };
-// One warp: the list's distribution and the student's logits at its classes (read before anything is written in place).
-// Returns the list's mass: 1, or 0 where it holds nothing.
+struct Entry {                       // one entry of the list, with the student's logit at its class
+    int id;
+    float t, v;
+    __device__ __forceinline__ bool holds() const { return id >= 0 && !(t == ninf()); }
+};
 template <typename T>
-__device__ __forceinline__ float read_teacher(const DistillArgs& p, int64_t row, Teacher& t, int lane)
+__device__ __forceinline__ Entry read_entry(const DistillArgs& p, const T* x, int64_t row, int j)
 {
-    const T* x = reinterpret_cast<const T*>(p.logits) + row * p.ld;
+    const int id = p.ids[row * p.k + j];
+    const float t = p.teacher[row * p.k + j];
+    const bool there = id >= 0 && id < p.n;
+    return Entry{there ? id : -1, there ? t : ninf(), there ? Io<T>::get(x[id]) : 0.f};
+}
+__device__ __forceinline__ void put_entry(Teacher& t, int j, const Entry& e)
+{
+    t.id[j] = e.id;
+    t.ln_q[j] = e.t;
+    t.v[j] = e.v;
+}
+// One warp: the distribution over the list, from its logits.
+__device__ __forceinline__ void list_distribution(const DistillArgs& p, Teacher& t, int lane)
+{
     float m = ninf();
-    for (int j = lane; j < p.k; j += 32) {
-        const int id = p.ids[row * p.k + j];
-        const bool there = id >= 0 && id < p.n;
-        const float v = there ? p.teacher[row * p.k + j] : ninf();
-        t.id[j] = there ? id : -1;
-        t.ln_q[j] = v;
-        t.v[j] = there ? Io<T>::get(x[id]) : 0.f;
-        m = v > m ? v : m;
-    }
+    for (int j = lane; j < p.k; j += 32) m = fmaxf(m, t.ln_q[j]);
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    const float base = m == ninf() ? 0.f : m;
+    const float base = base_of(m);
     float s = 0.f;
     for (int j = lane; j < p.k; j += 32) {
         const float u = (t.ln_q[j] - base) * p.inv_t;
@@ -659,38 +845,34 @@ __device__ __forceinline__ float read_teacher(const DistillArgs& p, int64_t row,
         t.ln_q[j] -= ln_s;
     }
     __syncwarp();
-    return none ? 0.f : 1.f;
 }
+// p_T of a class = 2^((v - m) c) / s, p = 2^((v - m1) log2 e) / h
 struct RowStats {
-    float m, l2s, l2h;               // log2-sum-exp around m at the temperature and at 1
+    float m, s, m1, h;
     bool none;
 };
 // One warp: the row's loss.
 __device__ __forceinline__ float distill_loss(const DistillArgs& p, const Teacher& t, float label_v, bool label_there, const RowStats& st, int lane)
 {
     if (st.none) return 0.f;
-    const float ln_s = st.l2s * kLn2;
+    const float ln_s = logf(st.s);
     float a = 0.f;
     for (int j = lane; j < p.k; j += 32)
         if (!(t.q[j] == 0.f)) a += t.q[j] * (t.ln_q[j] - ((t.v[j] - st.m) * p.inv_t - ln_s));
 #pragma unroll
     for (int d = 16; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
     float loss = p.alpha > 0.f ? p.alpha * p.temp * p.temp * a : 0.f;
-    if (p.alpha < 1.f && label_there) loss -= (1.f - p.alpha) * ((label_v - st.m) - st.l2h * kLn2);
+    if (p.alpha < 1.f && label_there) loss -= (1.f - p.alpha) * ((label_v - st.m1) - logf(st.h));
     return loss;
 }
-template <bool HARD>
-__device__ __forceinline__ RowStats stats_of(const Sums& a)
-{
-    return RowStats{base_of(a.m), log2f(a.s), HARD ? log2f(a.h) : 0.f, a.m == ninf() && a.s == 0.f};
-}
+__device__ __forceinline__ RowStats stats_of(const Sums& a) { return RowStats{base_of(a.m), a.s, base_of(a.m), a.h, a.m == ninf() && a.s == 0.f}; }
 template <bool HARD>
 __device__ __forceinline__ void write_loss(const DistillArgs& p, int64_t row, const RowStats& st, float loss)
 {
     p.loss[row] = loss;
     if (p.stats) {
-        p.stats[2 * row] = st.none ? ninf() : fmaf(st.m, p.inv_t, st.l2s * kLn2);
-        p.stats[2 * row + 1] = st.none ? ninf() : HARD ? fmaf(st.l2h, kLn2, st.m) : 0.f;
+        p.stats[2 * row] = st.none ? ninf() : fmaf(st.m, p.inv_t, logf(st.s));
+        p.stats[2 * row + 1] = st.none ? ninf() : HARD ? st.m1 + logf(st.h) : 0.f;
     }
 }
 // saved statistics, and whether they say enough (see RowScale)
@@ -698,29 +880,42 @@ __device__ __forceinline__ RowStats read_stats(const DistillArgs& p, int64_t row
 {
     const float a = p.stats[2 * row], b = p.stats[2 * row + 1];
     *enough = fabsf(a) < kLseExact && fabsf(b) < kLseExact;
-    return RowStats{0.f, a * kLog2e, b * kLog2e, false};
+    return RowStats{a * p.temp, 1.f, b, 1.f, false};
 }
 struct DistillGrad {                 // of one row: what every class gets, and what the listed ones get on top
-    float c, m, l2s, l2h, soft, hard, w;
+    float c, m, m1, soft, hard, power_hard, w, label;
     bool dead;                       // no distribution, or a weight of 0: zeros, whatever the logits hold
-    __device__ __forceinline__ DistillGrad(const DistillArgs& p, const RowStats& st, float d_loss, float mass, bool label_there)
+    __device__ __forceinline__ DistillGrad(const DistillArgs& p, const RowStats& st, float d_loss, bool list_there, bool label_there)
     {
         w = d_loss;
         dead = st.none || d_loss == 0.f;
         c = p.inv_t * kLog2e;
         m = st.m;
-        l2s = st.l2s;
-        l2h = st.l2h;
-        soft = p.alpha * p.temp * mass * w;
-        hard = label_there ? (1.f - p.alpha) * w : 0.f;
+        m1 = st.m1;
+        label = label_there ? (1.f - p.alpha) * w : 0.f;
+        soft = list_there ? p.alpha * p.temp * w / st.s : 0.f;
+        hard = label / st.h;
+        // p = (2^((v - m) c))^T 2^((m - m1) log2 e) / h; with a saved lse m - m1 is below (T - 1) ln n
+        power_hard = hard * ex2((m - m1) * kLog2e);
     }
     template <bool HARD>
     __device__ __forceinline__ float value(float v) const
     {
-        const float u = v - m;
-        float g = soft * ex2(fmaf(u, c, -l2s));
-        if (HARD) g = fmaf(hard, ex2(fmaf(u, kLog2e, -l2h)), g);
+        float g = soft * ex2((v - m) * c);
+        if (HARD) g = fmaf(hard, ex2((v - m1) * kLog2e), g);
         return g;
+    }
+    template <int POWER>
+    __device__ __forceinline__ f2 two(f2 v) const
+    {
+        const f2 e = ex2_2(mul2(add2(v, pair(-m, -m)), pair(c, c)));
+        const f2 a = pair(soft, soft), b = POWER == kOwnExp ? pair(hard, hard) : pair(power_hard, power_hard);
+        if (POWER == kNoHard) return mul2(a, e);
+        if (POWER == 1) return mul2(add2(a, b), e);
+        if (POWER == 2) return mul2(fma2(b, e, a), e);
+        if (POWER == 3) return mul2(fma2(b, mul2(e, e), a), e);
+        if (POWER == 4) return mul2(fma2(b, mul2(mul2(e, e), e), a), e);
+        return fma2(b, ex2_2(mul2(add2(v, pair(-m1, -m1)), pair(kLog2e, kLog2e))), mul2(a, e));
     }
 };
 // Classes of the list and the label, written again with what they get on top.  A class listed twice gets both weights: every one of its
@@ -733,64 +928,78 @@ __device__ __forceinline__ void write_listed(const DistillArgs& p, const Teacher
         const int id = t.id[j];
         if (id < 0 || !mine(id)) continue;
         float q = 0.f;
+#pragma unroll 8
         for (int i = 0; i < p.k; ++i) q += t.id[i] == id ? t.q[i] : 0.f;
         float v = g.value<HARD>(t.v[j]) - per_q * q;
-        if (HARD && id == label) v -= g.hard;
+        if (HARD && id == label) v -= g.label;
         out[id] = Io<T>::put(v);
     }
-    if (HARD && tid == 0 && label >= 0 && mine(label)) {
+    if (HARD && tid == threads - 1 && label >= 0 && mine(label)) {
         float q = 0.f;
+#pragma unroll 8
         for (int i = 0; i < p.k; ++i) q += t.id[i] == label ? t.q[i] : 0.f;
-        out[label] = Io<T>::put(g.value<HARD>(label_v) - per_q * q - g.hard);
+        out[label] = Io<T>::put(g.value<HARD>(label_v) - per_q * q - g.label);
     }
 }
 
 // FWD: the statistics are formed here (and the loss written); BWD: the gradient is written.  Both: the second reading of
-// the row comes from L2, which holds the rows in work (one per CTA).
+// the row comes from L2, which holds the rows in work (see rows_per_sm).
 template <typename T, int NT, bool HARD, bool FWD, bool BWD>
 __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) distill_kernel(const __grid_constant__ DistillArgs p)
 {
     __shared__ Sums s_part[32];
-    __shared__ Sums s_mine;
+    __shared__ Sums s_parts[kMaxParts];
     __shared__ Teacher s_teacher;
-    __shared__ float s_mass;
     const int part = (int)(blockIdx.x % (unsigned)p.parts);
     const int64_t row = blockIdx.x / (unsigned)p.parts;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const T* x = reinterpret_cast<const T*>(p.logits) + row * p.ld;
     const Share<T> sh(x, p.n, part, p.parts);
+    const float c = p.inv_t * kLog2e;
+    // the list and the student's logits at its classes come in while the row is gone over (kMaxTeacher <= NT)
+    Entry entry{-1, ninf(), 0.f};
+    if ((int)threadIdx.x < p.k) entry = read_entry<T>(p, x, row, threadIdx.x);
     const int label = HARD ? p.labels[row] : -1;
     const bool there = HARD && label >= 0 && label < p.n;
     const float label_v = there ? Io<T>::get(x[label]) : 0.f;
-    if (warp == 0) {
-        const float mass = read_teacher<T>(p, row, s_teacher, lane);
-        if (lane == 0) s_mass = mass;
-    }
-    const float c = p.inv_t * kLog2e;
+    const float d_loss = BWD ? p.d_loss[row] : 0.f;
     RowStats st;
-    bool again = FWD;
-    if constexpr (FWD) {
-        st = stats_of<HARD>(block_sums<NT, false, HARD>(run_over<T, NT, false, HARD>(sh, c, threadIdx.x), c, p.parts, s_part, &s_mine));
-        if (part == 0 && warp == 0) {
+    bool form = FWD;                         // the same for every part of a row
+    if constexpr (!FWD) {
+        bool enough;
+        st = read_stats(p, row, &enough);
+        form = !enough;
+    }
+    Sums a{ninf(), 0.f, 0.f, 0.f};
+    if (form) a = run_over_power<T, NT, HARD>(sh, c, threadIdx.x, p.power);
+    if ((int)threadIdx.x < p.k) put_entry(s_teacher, threadIdx.x, entry);
+    const bool list_there = __syncthreads_or(entry.holds());
+    if (form) {
+        a = block_sums<NT, false, HARD>(a, c, s_part);
+        if (p.parts > 1) a = cluster_sums<HARD>(a, c, part, p.parts, s_parts);
+        st = stats_of(a);
+    }
+    if (warp == 0) {
+        list_distribution(p, s_teacher, lane);
+        if (FWD && part == 0) {
             const float loss = distill_loss(p, s_teacher, label_v, there, st, lane);
             if (lane == 0) write_loss<HARD>(p, row, st, loss);
         }
-    } else {
-        bool enough;                 // the same for every part of a row
-        st = read_stats(p, row, &enough);
-        again = !enough;
-        if (again) st = stats_of<HARD>(block_sums<NT, false, HARD>(run_over<T, NT, false, HARD>(sh, c, threadIdx.x), c, p.parts, s_part, &s_mine));
     }
     if constexpr (BWD) {
-        __syncthreads();
-        const DistillGrad g(p, st, p.d_loss[row], s_mass, there);
+        const DistillGrad g(p, st, d_loss, list_there, there);
         T* out = reinterpret_cast<T*>(p.d_logits) + row * p.ld_d;
-        write_row<T, NT>(sh, out, threadIdx.x, [&](float v, int) { return g.dead ? 0.f : g.value<HARD>(v); });
+        if (g.dead) write_row<T, NT, false>(sh, out, threadIdx.x, [](f2) { return (f2)0; });
+        else if (!HARD) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<kNoHard>(v); });
+        else if (p.power == 1) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<1>(v); });
+        else if (p.power == 2) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<2>(v); });
+        else if (p.power == 3) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<3>(v); });
+        else if (p.power == 4) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<4>(v); });
+        else write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<kOwnExp>(v); });
         __syncthreads();
         if (!g.dead)
             write_listed<T, HARD>(p, s_teacher, g, there ? label : -1, label_v, out, threadIdx.x, NT, [&](int cls) { return sh.mine(cls); });
     }
-    if (again && p.parts > 1) cg::this_cluster().sync();
 }
 
 // A warp per row of at most 32 J classes.
@@ -812,7 +1021,14 @@ __global__ void __launch_bounds__(128) distill_warp_kernel(const __grid_constant
         v[j] = lane + 32 * j < p.n ? Io<T>::get(x[lane + 32 * j]) : ninf();
         m = fmaxf(m, v[j]);
     }
-    const float mass = read_teacher<T>(p, row, s_teacher[warp], lane);
+    bool holds = false;
+    for (int j = lane; j < p.k; j += 32) {
+        const Entry e = read_entry<T>(p, x, row, j);
+        put_entry(s_teacher[warp], j, e);
+        holds = holds || e.holds();
+    }
+    const bool list_there = __any_sync(0xffffffffu, holds);
+    list_distribution(p, s_teacher[warp], lane);
     const float c = p.inv_t * kLog2e;
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
@@ -823,14 +1039,14 @@ __global__ void __launch_bounds__(128) distill_warp_kernel(const __grid_constant
         Sums a{m, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < J; ++j) add_value<false, HARD>(a, v[j], c, base_of(m));
-        st = stats_of<HARD>(warp_sums<false, HARD>(a, c));
+        st = stats_of(warp_sums<false, HARD>(a, c));
     }
     if constexpr (FWD) {
         const float loss = distill_loss(p, s_teacher[warp], label_v, there, st, lane);
         if (lane == 0) write_loss<HARD>(p, row, st, loss);
     }
     if constexpr (BWD) {
-        const DistillGrad g(p, st, p.d_loss[row], mass, there);
+        const DistillGrad g(p, st, p.d_loss[row], list_there, there);
         T* out = reinterpret_cast<T*>(p.d_logits) + row * p.ld_d;
         __syncwarp();
 #pragma unroll
@@ -926,6 +1142,7 @@ int check_rows(const void* logits, int64_t rows, int32_t classes, int64_t ld, in
     if (rows && (!logits || !on(logits, element(dtype)))) return api_fail(HPF_ERR_INVALID, "logits: null or not aligned to their type");
     return HPF_OK;
 }
+int power_of(float temperature) { return temperature == 1.f ? 1 : temperature == 2.f ? 2 : temperature == 3.f ? 3 : temperature == 4.f ? 4 : 0; }
 int check_distill(const void* logits, const int32_t* labels, const int32_t* ids, const float* teacher, int64_t rows, int32_t classes, int64_t ld,
                   int32_t k, float temperature, float alpha, int32_t dtype)
 {
@@ -993,7 +1210,7 @@ extern "C" int hpf_distill_fwd(const void* d_logits, const int32_t* d_labels, co
     if (bad != HPF_OK) return bad;
     if (rows == 0) return HPF_OK;
     if (!d_loss) return api_fail(HPF_ERR_INVALID, "null argument");
-    DistillArgs a{d_logits, d_labels, d_teacher_ids, d_teacher_logits, d_loss, d_stats, nullptr, nullptr, rows, ld, 0, classes, k, 1, temperature, 1.f / temperature, alpha};
+    DistillArgs a{d_logits, d_labels, d_teacher_ids, d_teacher_logits, d_loss, d_stats, nullptr, nullptr, rows, ld, 0, classes, k, 1, temperature, 1.f / temperature, alpha, power_of(temperature)};
     return distill_call<true, false>(a, dtype, stream);
 }
 
@@ -1006,7 +1223,7 @@ extern "C" int hpf_distill_bwd(const void* d_logits, const int32_t* d_labels, co
     if (ld_d < classes) return api_fail(HPF_ERR_INVALID, "a row stride below the class count");
     if (rows == 0) return HPF_OK;
     if (!d_stats || !d_dloss || !d_dlogits || !on(d_dlogits, element(dtype))) return api_fail(HPF_ERR_INVALID, "null argument");
-    DistillArgs a{d_logits, d_labels, d_teacher_ids, d_teacher_logits, nullptr, const_cast<float*>(d_stats), d_dloss, d_dlogits, rows, ld, ld_d, classes, k, 1, temperature, 1.f / temperature, alpha};
+    DistillArgs a{d_logits, d_labels, d_teacher_ids, d_teacher_logits, nullptr, const_cast<float*>(d_stats), d_dloss, d_dlogits, rows, ld, ld_d, classes, k, 1, temperature, 1.f / temperature, alpha, power_of(temperature)};
     return distill_call<false, true>(a, dtype, stream);
 }
 
@@ -1019,6 +1236,6 @@ extern "C" int hpf_distill_fwd_bwd(const void* d_logits, const int32_t* d_labels
     if (ld_d < classes) return api_fail(HPF_ERR_INVALID, "a row stride below the class count");
     if (rows == 0) return HPF_OK;
     if (!d_loss || !d_dloss || !d_dlogits || !on(d_dlogits, element(dtype))) return api_fail(HPF_ERR_INVALID, "null argument");
-    DistillArgs a{d_logits, d_labels, d_teacher_ids, d_teacher_logits, d_loss, nullptr, d_dloss, d_dlogits, rows, ld, ld_d, classes, k, 1, temperature, 1.f / temperature, alpha};
+    DistillArgs a{d_logits, d_labels, d_teacher_ids, d_teacher_logits, d_loss, nullptr, d_dloss, d_dlogits, rows, ld, ld_d, classes, k, 1, temperature, 1.f / temperature, alpha, power_of(temperature)};
     return distill_call<true, true>(a, dtype, stream);
 }
