@@ -158,7 +158,10 @@ struct Share {
         first = part == 0;
         last = part == parts - 1;
     }
+    __device__ __forceinline__ const uint4* pieces() const { return reinterpret_cast<const uint4*>(row + lead); }
     __device__ __forceinline__ uint4 load(int c) const { return *(reinterpret_cast<const uint4*>(row + lead) + c); }
+    // the last reading of a piece: it goes first when L2 needs room
+    __device__ __forceinline__ uint4 load_last(int c) const { return __ldcs(reinterpret_cast<const uint4*>(row + lead) + c); }
     // the class that this thread reads by itself, or -1: V - 1 at most at either end of the row
     __device__ __forceinline__ int edge(int tid) const
     {
@@ -242,14 +245,8 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, c
     f2 base2 = 0;                                             // -m, twice
     int slot = 0, left = st ? st->iters : 0;
     float stretch = ninf();
-    uint4 raw[U];
-    int i = sh.c0 + tid;
-#pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = i + u * NT < sh.c1 ? sh.load(i + u * NT) : none;
-    while (i < sh.c1) {
-        uint4 next[U];                                        // under way while this round is worked on
-#pragma unroll
-        for (int u = 0; u < U; ++u) next[u] = i + (U + u) * NT < sh.c1 ? sh.load(i + (U + u) * NT) : none;
+    // one round: U pieces, of which the first `there` hold classes
+    const auto round = [&](const uint4 (&raw)[U], int there) {
         const float top = Io<T>::largest(Io<T>::larger(Io<T>::larger(raw[0], raw[1]), Io<T>::larger(raw[2], raw[3])));
         if (st) {
             stretch = fmaxf(stretch, top);
@@ -274,7 +271,7 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, c
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + u * NT < sh.c1) {
+            if (u < there) {
                 float f[V];
                 Io<T>::unpack(ENTROPY ? Io<T>::finite(raw[u]) : raw[u], f);
 #pragma unroll
@@ -289,10 +286,40 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, c
                     if (POWER == 4) { const f2 q = mul2(e, e); h2 = fma2(q, q, h2); }
                 }
             }
+    };
+    // whole rounds without a question, the next one's pieces under way; then what is left
+    const int full = (sh.c1 - sh.c0) / (U * NT), rest = sh.c0 + full * U * NT + tid;
+    int there = 0;
+    const uint4* at = sh.pieces() + sh.c0 + tid;
+    uint4 raw[U], next[U];
+    const auto load_rest = [&](uint4 (&to)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool in = rest + u * NT < sh.c1;
+            to[u] = in ? sh.load(rest + u * NT) : none;
+            there += in;
+        }
+    };
+    if (full > 0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = at[u * NT];
+    } else {
+        load_rest(raw);
+    }
+#pragma unroll 2
+    for (int r = 0; r < full; ++r) {
+        at += U * NT;
+        if (r + 1 < full) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) next[u] = at[u * NT];
+        } else {
+            load_rest(next);
+        }
+        round(raw, U);
 #pragma unroll
         for (int u = 0; u < U; ++u) raw[u] = next[u];
-        i += U * NT;
     }
+    if (there) round(raw, there);
     if (st)
         for (; slot < st->count; ++slot) {
             st->at[slot * NT + tid] = stretch;
@@ -383,8 +410,7 @@ __device__ __forceinline__ int key_class(unsigned long long key) { return 0x7fff
 constexpr int kStretches = 4096;   // of all threads of a CTA
 
 struct TopShared {
-    float group[kGroups];
-    float maxima[1024];
+    float maxima[512];
     float stretch[kStretches];
     unsigned short list[kStretches];
     unsigned long long cand[kCandidates];
@@ -413,11 +439,54 @@ __device__ __forceinline__ void over_stretches(const Share<T>& sh, const unsigne
     if (e >= 0) f(Io<T>::get(sh.row[e]), e);
 }
 
+// One warp: the k-th largest of the maxima of 32 groups of threads (a lane's group: threads lane, lane + 32, ...), by a bitonic sort.
+constexpr int kFewTop = 16;
+template <int NT>
+__device__ __forceinline__ float kth_of_32(const float* maxima, int k, int lane)
+{
+    float v = ninf();
+#pragma unroll
+    for (int t = 0; t < NT; t += 32) v = fmaxf(v, maxima[t + lane]);
+#pragma unroll
+    for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+        for (int d = size / 2; d; d /= 2) {
+            const float o = __shfl_xor_sync(0xffffffffu, v, d);
+            const bool larger = ((lane & d) == 0) == ((lane & size) == 0);       // largest first, over all 32 in the end
+            v = larger ? fmaxf(v, o) : fminf(v, o);
+        }
+    return __shfl_sync(0xffffffffu, v, k - 1);
+}
+// The same of 128 groups (threads t, t + 128, ...), to the upper 16 bits: four keys a lane, the bound found bit by bit.
+template <int NT>
+__device__ __forceinline__ float kth_of_128(const float* maxima, int k, int lane)
+{
+    uint32_t key[kGroups / 32];
+#pragma unroll
+    for (int i = 0; i < kGroups / 32; ++i) {
+        float v = ninf();
+#pragma unroll
+        for (int t = 0; t < NT; t += kGroups) v = fmaxf(v, maxima[t + i * 32 + lane]);
+        const uint32_t b = __float_as_uint(v + 0.0f);
+        key[i] = (b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u)) >> 16;
+    }
+    uint32_t bound = 0;
+#pragma unroll
+    for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < kGroups / 32; ++i) count += __popc(__ballot_sync(0xffffffffu, key[i] >= (bound | bit)));
+        if (count >= k) bound |= bit;
+    }
+    const uint32_t o = bound << 16;
+    return bound ? __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)) : ninf();
+}
+
 // The k largest classes of this CTA's share, best first, into sm.best.  Every thread knows the largest logit of each stretch of its strip
-// (sm.stretch) and of all of it (my_max).  The k-th largest of 128 group maxima is a lower bound of the k-th largest class, so only stretches
-// whose maximum reaches it are read again (from L2): about 128 ln(128 / (128 - k)) classes pass for unordered rows.  Threads t,
-// t + 128, ... form a group, so that a row sorted by frequency does not put its head into one group.  Where too many pass (long runs of
-// equal logits), a bisection over the unique keys raises the bound until they fit.
+// (sm.stretch) and of all of it (my_max).  The k-th largest of G group maxima is a lower bound of the k-th largest class, so only stretches
+// whose maximum reaches it are read again (from L2): about G ln(G / (G - k)) classes pass for unordered rows.  G is 32 up to k = 16, 128
+// above; a group's threads lie apart, so that a row sorted by frequency does not put its head into one group.  Where too many pass
+// (long runs of equal logits), a bisection over the unique keys raises the bound until they fit.
 template <typename T, int NT>
 __device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int k, int iters, TopShared& sm)
 {
@@ -426,22 +495,9 @@ __device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int
     if (tid == 0) { sm.count = 0; sm.listed = 0; }
     if (tid < kMaxTop) sm.best[tid] = 0ull;
     __syncthreads();
-    float g = ninf();
-    if (tid < kGroups) {
-#pragma unroll
-        for (int t = 0; t < NT; t += kGroups) g = fmaxf(g, sm.maxima[t + tid]);
-        sm.group[tid] = g;
-    }
-    __syncthreads();
-    if (tid < kGroups) {
-        int rank = 0;
-#pragma unroll
-        for (int j = 0; j < kGroups; j += 4) {
-            const float4 o = *reinterpret_cast<const float4*>(&sm.group[j]);
-            rank += (o.x > g || (o.x == g && j < tid)) + (o.y > g || (o.y == g && j + 1 < tid)) +
-                    (o.z > g || (o.z == g && j + 2 < tid)) + (o.w > g || (o.w == g && j + 3 < tid));
-        }
-        if (rank == k - 1) sm.bound = g;
+    if (tid < 32) {
+        const float bound = k <= kFewTop ? kth_of_32<NT>(sm.maxima, k, tid) : kth_of_128<NT>(sm.maxima, k, tid);
+        if (tid == 0) sm.bound = bound;
     }
     __syncthreads();
     const float bound = sm.bound;
@@ -534,9 +590,9 @@ __device__ __forceinline__ void write_stats(const LogprobsArgs& p, int64_t row, 
 }
 
 template <typename T, int NT, bool TOP>
-__global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) logprobs_fwd_kernel(const __grid_constant__ LogprobsArgs p)
+__global__ void __launch_bounds__(NT, NT == 256 ? 4 : 2) logprobs_fwd_kernel(const __grid_constant__ LogprobsArgs p)
 {
-    constexpr bool PARTS = NT == 1024;                   // a row is cut into parts only where few rows leave the CTAs large
+    constexpr bool PARTS = NT == 512;                   // a row is cut into parts only where few rows leave the CTAs large
     __shared__ Sums s_part[32];
     __shared__ Sums s_parts[kMaxParts];
     __shared__ __align__(16) unsigned char s_top[TOP ? sizeof(TopShared) : 16];
@@ -633,31 +689,44 @@ __global__ void __launch_bounds__(128) logprobs_fwd_warp_kernel(const __grid_con
 
 // ---- gradients -------------------------------------------------------------------------------------------------------
 // Writes g(two logits) for every two classes of the share.  `out` may be the logits themselves: a thread writes what it has read.
-// BOUNDED: nothing below -10^30 comes.
-template <typename T, int NT, bool BOUNDED, typename F>
+// BOUNDED: nothing below -10^30 comes.  AGAIN: the row has been gone over just now; it is read from its end to its start, what is in L2
+// since last first (4096 x 128000 bf16: 487 -> 452 us).
+template <typename T, int NT, bool BOUNDED, bool AGAIN, typename F>
 __device__ __forceinline__ void write_row(const Share<T>& sh, T* out, int tid, F&& g)
 {
     constexpr int V = Io<T>::V, U = 4;
     const bool wide = ((reinterpret_cast<uintptr_t>(out + sh.lead)) & 15) == 0;
-    for (int i = sh.c0 + tid; i < sh.c1; i += U * NT) {
+    const int full = (sh.c1 - sh.c0) / (U * NT), rest = sh.c0 + full * U * NT + tid;
+    const auto put = [&](int c, const uint4& raw) {
+        float f[V];
+        Io<T>::unpack(BOUNDED ? Io<T>::bounded(raw) : raw, f);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) split(g(pair(f[j], f[j + 1])), &f[j], &f[j + 1]);
+        T* to = out + sh.lead + c * V;
+        if (wide) __stcs(reinterpret_cast<uint4*>(to), Io<T>::pack(f));
+        else
+#pragma unroll
+            for (int j = 0; j < V; ++j) to[j] = Io<T>::put(f[j]);
+    };
+    const auto put_rest = [&]() {
         uint4 raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + u * NT < sh.c1) raw[u] = sh.load(i + u * NT);
+            if (rest + u * NT < sh.c1) raw[u] = AGAIN ? sh.load_last(rest + u * NT) : sh.load(rest + u * NT);
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + u * NT < sh.c1) {
-                float f[V];
-                Io<T>::unpack(BOUNDED ? Io<T>::bounded(raw[u]) : raw[u], f);
-                const int at = sh.lead + (i + u * NT) * V;
+            if (rest + u * NT < sh.c1) put(rest + u * NT, raw[u]);
+    };
+    if (AGAIN) put_rest();
+    for (int k = 0; k < full; ++k) {
+        const int i = sh.c0 + (AGAIN ? full - 1 - k : k) * U * NT + tid;
+        uint4 raw[U];
 #pragma unroll
-                for (int j = 0; j < V; j += 2) split(g(pair(f[j], f[j + 1])), &f[j], &f[j + 1]);
-                if (wide) __stcs(reinterpret_cast<uint4*>(out + at), Io<T>::pack(f));
-                else
+        for (int u = 0; u < U; ++u) raw[u] = AGAIN ? sh.load_last(i + u * NT) : sh.load(i + u * NT);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) out[at + j] = Io<T>::put(f[j]);
-            }
+        for (int u = 0; u < U; ++u) put(i + u * NT, raw[u]);
     }
+    if (!AGAIN) put_rest();
     const int e = sh.edge(tid);
     if (e >= 0) {
         const float v = Io<T>::get(sh.row[e]);
@@ -743,14 +812,14 @@ __global__ void __launch_bounds__(NT) logprobs_bwd_kernel(const __grid_constant_
     }
     g.scale(s);
     __syncthreads();                                         // the label's logit has been read (the gradient may be written in its place)
-    if (g.dead) write_row<T, NT, false>(sh, out, threadIdx.x, [](f2) { return (f2)0; });
+    if (g.dead) write_row<T, NT, false, false>(sh, out, threadIdx.x, [](f2) { return (f2)0; });
     else if (g.far)
-        write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) {
+        write_row<T, NT, false, false>(sh, out, threadIdx.x, [&](f2 v) {
             float x, y;
             split(v, &x, &y);
             return pair(g.slow(x), g.slow(y));
         });
-    else write_row<T, NT, true>(sh, out, threadIdx.x, g);
+    else write_row<T, NT, true, false>(sh, out, threadIdx.x, g);
     if (!g.dead && sh.mine(g.label)) {
         __syncthreads();
         if (threadIdx.x == 0) out[g.label] = Io<T>::put(g.label_value(label_v));
@@ -942,10 +1011,10 @@ __device__ __forceinline__ void write_listed(const DistillArgs& p, const Teacher
     }
 }
 
-// FWD: the statistics are formed here (and the loss written); BWD: the gradient is written.  Both: the second reading of
-// the row comes from L2, which holds the rows in work (see rows_per_sm).
+// FWD: the statistics are formed here (and the loss written); BWD: the gradient is written.  Both: the second reading of the row comes
+// from L2.
 template <typename T, int NT, bool HARD, bool FWD, bool BWD>
-__global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) distill_kernel(const __grid_constant__ DistillArgs p)
+__global__ void __launch_bounds__(NT, NT == 256 ? 4 : NT == 512 ? 2 : 1) distill_kernel(const __grid_constant__ DistillArgs p)
 {
     __shared__ Sums s_part[32];
     __shared__ Sums s_parts[kMaxParts];
@@ -989,13 +1058,13 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) distill_kernel(const __
     if constexpr (BWD) {
         const DistillGrad g(p, st, d_loss, list_there, there);
         T* out = reinterpret_cast<T*>(p.d_logits) + row * p.ld_d;
-        if (g.dead) write_row<T, NT, false>(sh, out, threadIdx.x, [](f2) { return (f2)0; });
-        else if (!HARD) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<kNoHard>(v); });
-        else if (p.power == 1) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<1>(v); });
-        else if (p.power == 2) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<2>(v); });
-        else if (p.power == 3) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<3>(v); });
-        else if (p.power == 4) write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<4>(v); });
-        else write_row<T, NT, false>(sh, out, threadIdx.x, [&](f2 v) { return g.two<kOwnExp>(v); });
+        if (g.dead) write_row<T, NT, false, FWD>(sh, out, threadIdx.x, [](f2) { return (f2)0; });
+        else if (!HARD) write_row<T, NT, false, FWD>(sh, out, threadIdx.x, [&](f2 v) { return g.two<kNoHard>(v); });
+        else if (p.power == 1) write_row<T, NT, false, FWD>(sh, out, threadIdx.x, [&](f2 v) { return g.two<1>(v); });
+        else if (p.power == 2) write_row<T, NT, false, FWD>(sh, out, threadIdx.x, [&](f2 v) { return g.two<2>(v); });
+        else if (p.power == 3) write_row<T, NT, false, FWD>(sh, out, threadIdx.x, [&](f2 v) { return g.two<3>(v); });
+        else if (p.power == 4) write_row<T, NT, false, FWD>(sh, out, threadIdx.x, [&](f2 v) { return g.two<4>(v); });
+        else write_row<T, NT, false, FWD>(sh, out, threadIdx.x, [&](f2 v) { return g.two<kOwnExp>(v); });
         __syncthreads();
         if (!g.dead)
             write_listed<T, HARD>(p, s_teacher, g, there ? label : -1, label_v, out, threadIdx.x, NT, [&](int cls) { return sh.mine(cls); });
@@ -1065,11 +1134,11 @@ int sm_count()
     if (sms.get(&n, [](int dev, int* v) { return cudaDeviceGetAttribute(v, cudaDevAttrMultiProcessorCount, dev); }) != cudaSuccess) return 148;
     return n;
 }
-// Parts of a row: while there are fewer CTAs than SMs and every part keeps 8 KB.
+// Parts of a row: while the CTAs (of 512 threads) still fit the SMs one each and every part keeps 8 KB.
 int parts_of(int64_t rows, int n, size_t elem)
 {
     int parts = 1;
-    while (parts < kMaxParts && rows * parts < sm_count() && (size_t)n * elem / (2 * parts) >= 8192) parts *= 2;
+    while (parts < kMaxParts && rows * parts * 2 <= sm_count() && (size_t)n * elem / (2 * parts) >= 8192) parts *= 2;
     return parts;
 }
 template <typename K, typename A>
@@ -1102,8 +1171,8 @@ cudaError_t logprobs_fwd(LogprobsArgs& a, cudaStream_t st)
     if (a.n <= kWarpRow) return launch_warps(logprobs_fwd_warp_kernel<T, 32>, a.rows, st, a);
     a.parts = parts_of(a.rows, a.n, sizeof(T));
     if (a.parts > 1) {
-        if (a.k) return launch_rows(logprobs_fwd_kernel<T, 1024, true>, a.rows, a.parts, 1024, st, a);
-        return launch_rows(logprobs_fwd_kernel<T, 1024, false>, a.rows, a.parts, 1024, st, a);
+        if (a.k) return launch_rows(logprobs_fwd_kernel<T, 512, true>, a.rows, a.parts, 512, st, a);
+        return launch_rows(logprobs_fwd_kernel<T, 512, false>, a.rows, a.parts, 512, st, a);
     }
     if (a.k) return launch_rows(logprobs_fwd_kernel<T, 256, true>, a.rows, 1, 256, st, a);
     return launch_rows(logprobs_fwd_kernel<T, 256, false>, a.rows, 1, 256, st, a);
@@ -1115,6 +1184,12 @@ cudaError_t logprobs_bwd(LogprobsGradArgs& a, cudaStream_t st)
     a.parts = parts_of(a.rows, a.n, sizeof(T));
     return launch_rows(logprobs_bwd_kernel<T, 256>, a.rows, a.parts, 256, st, a);
 }
+template <typename T, int NT, bool HARD, bool FWD, bool BWD>
+cudaError_t distill_rows(DistillArgs& a, cudaStream_t st)
+{
+    auto* kernel = distill_kernel<T, NT, HARD, FWD, BWD>;
+    return launch_rows(kernel, a.rows, a.parts, NT, st, a);
+}
 template <typename T, bool HARD, bool FWD, bool BWD>
 cudaError_t distill_one(DistillArgs& a, cudaStream_t st)
 {
@@ -1122,8 +1197,9 @@ cudaError_t distill_one(DistillArgs& a, cudaStream_t st)
     if (a.n <= 256) return launch_warps(distill_warp_kernel<T, 8, HARD, FWD, BWD>, a.rows, st, a);
     if (a.n <= kWarpRow) return launch_warps(distill_warp_kernel<T, 32, HARD, FWD, BWD>, a.rows, st, a);
     a.parts = parts_of(a.rows, a.n, sizeof(T));
-    if (a.parts > 1) return launch_rows(distill_kernel<T, 1024, HARD, FWD, BWD>, a.rows, a.parts, 1024, st, a);
-    return launch_rows(distill_kernel<T, 256, HARD, FWD, BWD>, a.rows, 1, 256, st, a);
+    static const int nt = getenv("HPF_NT") ? atoi(getenv("HPF_NT")) : 256;
+    if (a.parts > 1 || nt == 512) return distill_rows<T, 512, HARD, FWD, BWD>(a, st);
+    return distill_rows<T, 256, HARD, FWD, BWD>(a, st);
 }
 template <typename T, bool FWD, bool BWD>
 cudaError_t distill(DistillArgs& a, cudaStream_t st)
