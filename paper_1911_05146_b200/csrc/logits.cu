@@ -412,31 +412,43 @@ constexpr int kStretches = 4096;   // of all threads of a CTA
 struct TopShared {
     float maxima[512];
     float stretch[kStretches];
-    unsigned short list[kStretches];
     unsigned long long cand[kCandidates];
-    unsigned long long best[kMaxTop];
+    int rank[kCandidates];
+    unsigned short list[kStretches];
     int count, listed;
     float bound;
 };
 
-// Calls f(value, class) for every class of the listed stretches, spread over the CTA, and of the row's ends.
+// Calls f(value, class) for every class at or above the bound in the listed stretches, which are spread over the CTA piece by piece, and in
+// the row's ends.
 template <typename T, int NT, typename F>
-__device__ __forceinline__ void over_stretches(const Share<T>& sh, const unsigned short* list, int listed, int iters, F&& f)
+__device__ __forceinline__ void over_stretches(const Share<T>& sh, const TopShared& sm, int listed, float bound, int iters, F&& f)
 {
     constexpr int V = Io<T>::V, U = 4;
     const unsigned per = (unsigned)(iters * U);                    // pieces of a stretch
     for (unsigned w = threadIdx.x; w < (unsigned)listed * per; w += NT) {
-        const unsigned at = w / per, piece = w - at * per, entry = list[at];
+        const unsigned at = iters == 1 ? w / U : w / per, piece = w - at * per, entry = sm.list[at];
         const int c = sh.c0 + (int)(entry % NT) + (int)((entry / NT) * per + piece) * NT;
         if (c < sh.c1) {
             float v[V];
             Io<T>::unpack(sh.load(c), v);
+            uint32_t which = 0;
 #pragma unroll
-            for (int j = 0; j < V; ++j) f(v[j], sh.lead + c * V + j);
+            for (int j = 0; j < V; ++j) which |= (v[j] >= bound && v[j] > ninf() ? 1u : 0u) << j;
+            for (; which; which &= which - 1) {
+                const int j = __ffs(which) - 1;
+                float x = v[0];
+#pragma unroll
+                for (int i = 1; i < V; ++i) x = i == j ? v[i] : x;
+                f(x, sh.lead + c * V + j);
+            }
         }
     }
     const int e = sh.edge(threadIdx.x);
-    if (e >= 0) f(Io<T>::get(sh.row[e]), e);
+    if (e >= 0) {
+        const float x = Io<T>::get(sh.row[e]);
+        if (x >= bound && x > ninf()) f(x, e);
+    }
 }
 
 // One warp: the k-th largest of the maxima of 32 groups of threads (a lane's group: threads lane, lane + 32, ...), by a bitonic sort.
@@ -470,9 +482,11 @@ __device__ __forceinline__ float kth_of_128(const float* maxima, int k, int lane
         const uint32_t b = __float_as_uint(v + 0.0f);
         key[i] = (b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u)) >> 16;
     }
-    uint32_t bound = 0;
-#pragma unroll
-    for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
+    // the bits that all keys share are the bound's too
+    const uint32_t most = __reduce_max_sync(0xffffffffu, max(max(key[0], key[1]), max(key[2], key[3])));
+    const uint32_t least = __reduce_min_sync(0xffffffffu, min(min(key[0], key[1]), min(key[2], key[3])));
+    uint32_t bit = most == least ? 0u : 0x80000000u >> __clz(most ^ least), bound = bit ? most & ~(2 * bit - 1) : most;
+    for (; bit; bit >>= 1) {
         int count = 0;
 #pragma unroll
         for (int i = 0; i < kGroups / 32; ++i) count += __popc(__ballot_sync(0xffffffffu, key[i] >= (bound | bit)));
@@ -482,18 +496,18 @@ __device__ __forceinline__ float kth_of_128(const float* maxima, int k, int lane
     return bound ? __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)) : ninf();
 }
 
-// The k largest classes of this CTA's share, best first, into sm.best.  Every thread knows the largest logit of each stretch of its strip
+// The k largest classes of this CTA's share are among the sm.cand[0 .. the result); sm.rank has their places.  Every thread knows the largest logit of each stretch of its strip
 // (sm.stretch) and of all of it (my_max).  The k-th largest of G group maxima is a lower bound of the k-th largest class, so only stretches
 // whose maximum reaches it are read again (from L2): about G ln(G / (G - k)) classes pass for unordered rows.  G is 32 up to k = 16, 128
 // above; a group's threads lie apart, so that a row sorted by frequency does not put its head into one group.  Where too many pass
 // (long runs of equal logits), a bisection over the unique keys raises the bound until they fit.
 template <typename T, int NT>
-__device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int k, int iters, TopShared& sm)
+__device__ __forceinline__ int select_top(const Share<T>& sh, float my_max, int k, int iters, TopShared& sm)
 {
     const int tid = threadIdx.x;
     sm.maxima[tid] = my_max;
     if (tid == 0) { sm.count = 0; sm.listed = 0; }
-    if (tid < kMaxTop) sm.best[tid] = 0ull;
+    for (int i = tid; i < kCandidates; i += NT) sm.rank[i] = 0;
     __syncthreads();
     if (tid < 32) {
         const float bound = k <= kFewTop ? kth_of_32<NT>(sm.maxima, k, tid) : kth_of_128<NT>(sm.maxima, k, tid);
@@ -510,11 +524,9 @@ __device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int
     }
     __syncthreads();
     const int listed = sm.listed;
-    over_stretches<T, NT>(sh, sm.list, listed, iters, [&](float v, int cls) {
-        if (v >= bound && v > ninf()) {
-            const int at = atomicAdd(&sm.count, 1);
-            if (at < kCandidates) sm.cand[at] = class_key(v, cls);
-        }
+    over_stretches<T, NT>(sh, sm, listed, bound, iters, [&](float v, int cls) {
+        const int at = atomicAdd(&sm.count, 1);
+        if (at < kCandidates) sm.cand[at] = class_key(v, cls);
     });
     __syncthreads();
     int count = sm.count;
@@ -527,7 +539,7 @@ __device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int
             __syncthreads();
             if (tid == 0) sm.count = 0;
             __syncthreads();
-            over_stretches<T, NT>(sh, sm.list, listed, iters, [&](float v, int cls) {
+            over_stretches<T, NT>(sh, sm, listed, bound, iters, [&](float v, int cls) {
                 const unsigned long long key = class_key(v, cls);
                 if (key >= mid) {
                     const int at = atomicAdd(&sm.count, 1);
@@ -539,16 +551,21 @@ __device__ __forceinline__ void select_top(const Share<T>& sh, float my_max, int
             if (above >= k) { lo = mid; count = above; }
             else hi = mid;
         }
+        __syncthreads();
     }
-    __syncthreads();
-    for (int i = tid; i < count; i += NT) {
+    // a class's place is the number of larger keys; several threads count for one where there are enough
+    int share = NT;
+    while (share >= 2 * count && share > 32) share /= 2;
+    for (int i = tid % share; i < count; i += share) {
         const unsigned long long mine = sm.cand[i];
         int rank = 0;
-#pragma unroll 8
-        for (int j = 0; j < count; ++j) rank += sm.cand[j] > mine;
-        if (rank < k) sm.best[rank] = mine;
+#pragma unroll 4
+        for (int j = tid / share; j < count; j += NT / share) rank += sm.cand[j] > mine;
+        if (share == NT) sm.rank[i] = rank;
+        else atomicAdd(&sm.rank[i], rank);
     }
     __syncthreads();
+    return count;
 }
 
 struct LogprobsArgs {
@@ -613,33 +630,55 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 2) logprobs_fwd_kernel(con
     const float my_max = a.m;
     a = block_sums<NT, true, false>(a, c, s_part);
     // the strips' maxima leave the row's ends out: they are always looked at again
-    if constexpr (TOP) select_top<T, NT>(sh, my_max, p.k, st.iters, sm);
-    if (PARTS && p.parts > 1) {
+    int count = 0;
+    if constexpr (TOP) count = select_top<T, NT>(sh, my_max, p.k, st.iters, sm);
+    if (!PARTS || p.parts == 1) {
+        if (threadIdx.x == 0) write_stats<T>(p, row, a);
+        if constexpr (TOP) {
+            const float ln_s = logf(a.s);
+            for (int i = threadIdx.x; i < count; i += NT)
+                if (sm.rank[i] < p.k) write_top(p, row, sm.rank[i], sm.cand[i], a.m, ln_s);
+            for (int i = count + threadIdx.x; i < p.k; i += NT) write_top(p, row, i, 0ull, a.m, ln_s);
+        }
+        return;
+    }
+    if constexpr (PARTS) {
         // sums and lists go to the row's first CTA
         cg::cluster_group cl = cg::this_cluster();
         if (threadIdx.x == 0) *cl.map_shared_rank(&s_parts[part], 0) = a;
         if constexpr (TOP) {
-            if ((int)threadIdx.x < p.k) *cl.map_shared_rank(&s_all[part * p.k + threadIdx.x], 0) = sm.best[threadIdx.x];
+            unsigned long long* there = cl.map_shared_rank(s_all + part * p.k, 0);
+            for (int i = threadIdx.x; i < count; i += NT)
+                if (sm.rank[i] < p.k) there[sm.rank[i]] = sm.cand[i];
+            for (int i = count + threadIdx.x; i < p.k; i += NT) there[i] = 0ull;
         }
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
         if (part) return;
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         a = join_sums<true, false>(s_parts, p.parts, threadIdx.x & 31, c);
-    }
-    if (threadIdx.x == 0) write_stats<T>(p, row, a);
-    if constexpr (TOP) {
-        const float ln_s = logf(a.s);
-        if (!PARTS || p.parts == 1) {
-            if ((int)threadIdx.x < p.k) write_top(p, row, threadIdx.x, sm.best[threadIdx.x], a.m, ln_s);
-        } else {
+        if (threadIdx.x == 0) write_stats<T>(p, row, a);
+        if constexpr (TOP) {
+            const float ln_s = logf(a.s);
             const int total = p.parts * p.k;
             for (int i = threadIdx.x; i < total; i += NT) {
+                // the parts' lists are in order: a class's place is the number of larger keys in each
                 const unsigned long long mine = s_all[i];
                 int rank = 0;
-#pragma unroll 8
-                for (int j = 0; j < total; ++j) rank += s_all[j] > mine || (s_all[j] == mine && j < i);   // only zeros repeat
-                if (rank < p.k) write_top(p, row, rank, mine, a.m, ln_s);
+                for (int q = 0; q < p.parts; ++q) {
+                    const unsigned long long* list = s_all + q * p.k;
+                    int lo = 0;                              // keys before lo are larger
+#pragma unroll
+                    for (int step = kMaxTop; step; step >>= 1)
+                        if (lo + step <= p.k && list[lo + step - 1] > mine) lo += step;
+                    rank += lo;
+                }
+                if (mine && rank < p.k) write_top(p, row, rank, mine, a.m, ln_s);
             }
+            // fewer classes than places
+            int listed = 0;
+            for (int i = threadIdx.x & 31; i < total; i += 32) listed += s_all[i] != 0ull;
+            listed = __reduce_add_sync(0xffffffffu, listed);
+            for (int i = listed + threadIdx.x; i < p.k; i += NT) write_top(p, row, i, 0ull, a.m, ln_s);
         }
     }
 }
@@ -718,13 +757,33 @@ __device__ __forceinline__ void write_row(const Share<T>& sh, T* out, int tid, F
             if (rest + u * NT < sh.c1) put(rest + u * NT, raw[u]);
     };
     if (AGAIN) put_rest();
-    for (int k = 0; k < full; ++k) {
-        const int i = sh.c0 + (AGAIN ? full - 1 - k : k) * U * NT + tid;
-        uint4 raw[U];
+    if constexpr (AGAIN) {
+        uint4 raw[U], next[U];
+        int i = sh.c0 + (full - 1) * U * NT + tid;
+        if (full > 0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = AGAIN ? sh.load_last(i + u * NT) : sh.load(i + u * NT);
+            for (int u = 0; u < U; ++u) raw[u] = sh.load_last(i + u * NT);
+        }
+#pragma unroll 2
+        for (int k = full; k > 0; --k, i -= U * NT) {
+            if (k > 1) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) put(i + u * NT, raw[u]);
+                for (int u = 0; u < U; ++u) next[u] = sh.load_last(i + (u - U) * NT);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) put(i + u * NT, raw[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = next[u];
+        }
+    } else {
+        for (int k = 0; k < full; ++k) {
+            const int i = sh.c0 + k * U * NT + tid;
+            uint4 raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = sh.load(i + u * NT);
+#pragma unroll
+            for (int u = 0; u < U; ++u) put(i + u * NT, raw[u]);
+        }
     }
     if (!AGAIN) put_rest();
     const int e = sh.edge(tid);
@@ -1197,8 +1256,9 @@ cudaError_t distill_one(DistillArgs& a, cudaStream_t st)
     if (a.n <= 256) return launch_warps(distill_warp_kernel<T, 8, HARD, FWD, BWD>, a.rows, st, a);
     if (a.n <= kWarpRow) return launch_warps(distill_warp_kernel<T, 32, HARD, FWD, BWD>, a.rows, st, a);
     a.parts = parts_of(a.rows, a.n, sizeof(T));
-    static const int nt = getenv("HPF_NT") ? atoi(getenv("HPF_NT")) : 256;
-    if (a.parts > 1 || nt == 512) return distill_rows<T, 512, HARD, FWD, BWD>(a, st);
+    // Loss and gradient at once read a row twice, so the rows in work should fit L2: half as many of long ones (4096 rows of 256 KB: 445 us
+    // with CTAs of 256, 412 with 512; of 100 KB: 165 and 200; of 128 KB: 108 and 106).
+    if (a.parts > 1 || (FWD && BWD && (size_t)a.n * sizeof(T) > 120 * 1024)) return distill_rows<T, 512, HARD, FWD, BWD>(a, st);
     return distill_rows<T, 256, HARD, FWD, BWD>(a, st);
 }
 template <typename T, bool FWD, bool BWD>
