@@ -29,7 +29,7 @@ constexpr int kMaxTeacher = 256;   // entries of a teacher's list per row
 constexpr int kWarpRow = 1024;     // classes up to which a warp holds a row
 constexpr int kMaxParts = 8;       // CTAs a row is cut into (portable cluster size)
 constexpr int kGroups = 128;       // groups of threads whose maxima bound the k-th largest class
-constexpr int kCandidates = 1024;  // classes at or above that bound that are ranked by counting
+constexpr int kCandidates = 512;   // classes at or above that bound that are ranked by counting
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFloor = -1e30f;   // stands for -inf where it meets a weight of 0
 
@@ -220,6 +220,12 @@ __device__ __forceinline__ void add_value(Sums& a, float v, float c, float base)
 }
 __device__ __forceinline__ float base_of(float m) { return m == ninf() ? 0.f : m; }
 
+// The upper half of a logit's place among the floats: in their order, equal where the upper 16 bits are.
+__device__ __forceinline__ uint32_t order16(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return (b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) >> 16;
+}
 // Where a thread leaves the largest logit of each stretch of its strip (for the list of the largest classes).
 struct Stretches {
     float* at;           // [count][threads]
@@ -407,10 +413,10 @@ __device__ __forceinline__ float key_value(unsigned long long key)
 }
 __device__ __forceinline__ int key_class(unsigned long long key) { return 0x7fffffff - (int)(uint32_t)(key & 0xffffffffu); }
 
-constexpr int kStretches = 4096;   // of all threads of a CTA
-
+template <int NT>
 struct TopShared {
-    float maxima[512];
+    static constexpr int kStretches = (NT == 512 ? 8 : 16) * NT;
+    float maxima[NT];
     float stretch[kStretches];
     unsigned long long cand[kCandidates];
     int rank[kCandidates];
@@ -422,7 +428,7 @@ struct TopShared {
 // Calls f(value, class) for every class at or above the bound in the listed stretches, which are spread over the CTA piece by piece, and in
 // the row's ends.
 template <typename T, int NT, typename F>
-__device__ __forceinline__ void over_stretches(const Share<T>& sh, const TopShared& sm, int listed, float bound, int iters, F&& f)
+__device__ __forceinline__ void over_stretches(const Share<T>& sh, const TopShared<NT>& sm, int listed, float bound, int iters, F&& f)
 {
     constexpr int V = Io<T>::V, U = 4;
     const unsigned per = (unsigned)(iters * U);                    // pieces of a stretch
@@ -479,8 +485,7 @@ __device__ __forceinline__ float kth_of_128(const float* maxima, int k, int lane
         float v = ninf();
 #pragma unroll
         for (int t = 0; t < NT; t += kGroups) v = fmaxf(v, maxima[t + i * 32 + lane]);
-        const uint32_t b = __float_as_uint(v + 0.0f);
-        key[i] = (b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u)) >> 16;
+        key[i] = order16(v);
     }
     // the bits that all keys share are the bound's too
     const uint32_t most = __reduce_max_sync(0xffffffffu, max(max(key[0], key[1]), max(key[2], key[3])));
@@ -502,7 +507,7 @@ __device__ __forceinline__ float kth_of_128(const float* maxima, int k, int lane
 // above; a group's threads lie apart, so that a row sorted by frequency does not put its head into one group.  Where too many pass
 // (long runs of equal logits), a bisection over the unique keys raises the bound until they fit.
 template <typename T, int NT>
-__device__ __forceinline__ int select_top(const Share<T>& sh, float my_max, int k, int iters, TopShared& sm)
+__device__ __forceinline__ int select_top(const Share<T>& sh, float my_max, int k, int iters, TopShared<NT>& sm)
 {
     const int tid = threadIdx.x;
     sm.maxima[tid] = my_max;
@@ -517,7 +522,7 @@ __device__ __forceinline__ int select_top(const Share<T>& sh, float my_max, int 
     const float bound = sm.bound;
     if (my_max >= bound && my_max > ninf()) {
 #pragma unroll
-        for (int s = 0; s < kStretches / NT; ++s) {
+        for (int s = 0; s < TopShared<NT>::kStretches / NT; ++s) {
             const float v = sm.stretch[s * NT + tid];
             if (v >= bound && v > ninf()) sm.list[atomicAdd(&sm.listed, 1)] = (unsigned short)(s * NT + tid);
         }
@@ -607,23 +612,23 @@ __device__ __forceinline__ void write_stats(const LogprobsArgs& p, int64_t row, 
 }
 
 template <typename T, int NT, bool TOP>
-__global__ void __launch_bounds__(NT, NT == 256 ? 4 : 2) logprobs_fwd_kernel(const __grid_constant__ LogprobsArgs p)
+__global__ void __launch_bounds__(NT, 1024 / NT) logprobs_fwd_kernel(const __grid_constant__ LogprobsArgs p)
 {
     constexpr bool PARTS = NT == 512;                   // a row is cut into parts only where few rows leave the CTAs large
     __shared__ Sums s_part[32];
     __shared__ Sums s_parts[kMaxParts];
-    __shared__ __align__(16) unsigned char s_top[TOP ? sizeof(TopShared) : 16];
+    __shared__ __align__(16) unsigned char s_top[TOP ? sizeof(TopShared<NT>) : 16];
     __shared__ unsigned long long s_all[TOP && PARTS ? kMaxParts * kMaxTop : 1];
     const int part = PARTS ? (int)(blockIdx.x % (unsigned)p.parts) : 0;
     const int64_t row = PARTS ? blockIdx.x / (unsigned)p.parts : blockIdx.x;
     const float c = p.inv_t * kLog2e;
     const Share<T> sh(reinterpret_cast<const T*>(p.logits) + row * p.ld, p.n, part, PARTS ? p.parts : 1);
-    TopShared& sm = *reinterpret_cast<TopShared*>(s_top);
+    TopShared<NT>& sm = *reinterpret_cast<TopShared<NT>*>(s_top);
     Stretches st{nullptr, 0, 0};
     if (TOP) {
         const int rounds = (sh.c1 - sh.c0 + 4 * NT - 1) / (4 * NT);
         st.at = sm.stretch;
-        st.count = kStretches / NT;
+        st.count = TopShared<NT>::kStretches / NT;
         st.iters = (rounds + st.count - 1) / st.count;
     }
     Sums a = run_over<T, NT, true, kNoHard>(sh, c, threadIdx.x, TOP ? &st : nullptr);
@@ -1073,7 +1078,7 @@ __device__ __forceinline__ void write_listed(const DistillArgs& p, const Teacher
 // FWD: the statistics are formed here (and the loss written); BWD: the gradient is written.  Both: the second reading of the row comes
 // from L2.
 template <typename T, int NT, bool HARD, bool FWD, bool BWD>
-__global__ void __launch_bounds__(NT, NT == 256 ? 4 : NT == 512 ? 2 : 1) distill_kernel(const __grid_constant__ DistillArgs p)
+__global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const __grid_constant__ DistillArgs p)
 {
     __shared__ Sums s_part[32];
     __shared__ Sums s_parts[kMaxParts];
@@ -1084,9 +1089,15 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : NT == 512 ? 2 : 1) distill
     const T* x = reinterpret_cast<const T*>(p.logits) + row * p.ld;
     const Share<T> sh(x, p.n, part, p.parts);
     const float c = p.inv_t * kLog2e;
-    // the list and the student's logits at its classes come in while the row is gone over (kMaxTeacher <= NT)
-    Entry entry{-1, ninf(), 0.f};
-    if ((int)threadIdx.x < p.k) entry = read_entry<T>(p, x, row, threadIdx.x);
+    // the list and the student's logits at its classes come in while the row is gone over
+    constexpr int ENTRIES = (kMaxTeacher + NT - 1) / NT;
+    Entry entry[ENTRIES];
+    bool holds = false;
+#pragma unroll
+    for (int i = 0; i < ENTRIES; ++i) {
+        entry[i] = Entry{-1, ninf(), 0.f};
+        if ((int)threadIdx.x + i * NT < p.k) entry[i] = read_entry<T>(p, x, row, threadIdx.x + i * NT);
+    }
     const int label = HARD ? p.labels[row] : -1;
     const bool there = HARD && label >= 0 && label < p.n;
     const float label_v = there ? Io<T>::get(x[label]) : 0.f;
@@ -1100,8 +1111,12 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 4 : NT == 512 ? 2 : 1) distill
     }
     Sums a{ninf(), 0.f, 0.f, 0.f};
     if (form) a = run_over_power<T, NT, HARD>(sh, c, threadIdx.x, p.power);
-    if ((int)threadIdx.x < p.k) put_entry(s_teacher, threadIdx.x, entry);
-    const bool list_there = __syncthreads_or(entry.holds());
+#pragma unroll
+    for (int i = 0; i < ENTRIES; ++i) {
+        if ((int)threadIdx.x + i * NT < p.k) put_entry(s_teacher, threadIdx.x + i * NT, entry[i]);
+        holds = holds || entry[i].holds();
+    }
+    const bool list_there = __syncthreads_or(holds);
     if (form) {
         a = block_sums<NT, false, HARD>(a, c, s_part);
         if (p.parts > 1) a = cluster_sums<HARD>(a, c, part, p.parts, s_parts);
@@ -1215,6 +1230,10 @@ cudaError_t launch_rows(K* kernel, int64_t rows, int parts, int threads, cudaStr
     cfg.numAttrs = parts > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, args);
 }
+// Rows per SM from which CTAs of 128 threads take them: eight rows at different steps hide each other's waits better than four (4096 x 50021
+// bf16 with 8 listed classes: 94 -> 82 us; 100 rows: 8.7 -> 11 us).
+constexpr int kManyRows = 4;
+
 template <typename K, typename A>
 cudaError_t launch_warps(K* kernel, int64_t rows, cudaStream_t st, const A& args)
 {
@@ -1232,6 +1251,11 @@ cudaError_t logprobs_fwd(LogprobsArgs& a, cudaStream_t st)
     if (a.parts > 1) {
         if (a.k) return launch_rows(logprobs_fwd_kernel<T, 512, true>, a.rows, a.parts, 512, st, a);
         return launch_rows(logprobs_fwd_kernel<T, 512, false>, a.rows, a.parts, 512, st, a);
+    }
+    // (longer rows would have stretches of more than one round, 1.06 of the time with 256 threads at 256 KB)
+    if (a.rows >= kManyRows * sm_count() && (size_t)a.n * sizeof(T) <= TopShared<128>::kStretches * 64) {
+        if (a.k) return launch_rows(logprobs_fwd_kernel<T, 128, true>, a.rows, 1, 128, st, a);
+        return launch_rows(logprobs_fwd_kernel<T, 128, false>, a.rows, 1, 128, st, a);
     }
     if (a.k) return launch_rows(logprobs_fwd_kernel<T, 256, true>, a.rows, 1, 256, st, a);
     return launch_rows(logprobs_fwd_kernel<T, 256, false>, a.rows, 1, 256, st, a);
@@ -1257,8 +1281,9 @@ cudaError_t distill_one(DistillArgs& a, cudaStream_t st)
     if (a.n <= kWarpRow) return launch_warps(distill_warp_kernel<T, 32, HARD, FWD, BWD>, a.rows, st, a);
     a.parts = parts_of(a.rows, a.n, sizeof(T));
     // Loss and gradient at once read a row twice, so the rows in work should fit L2: half as many of long ones (4096 rows of 256 KB: 445 us
-    // with CTAs of 256, 412 with 512; of 100 KB: 165 and 200; of 128 KB: 108 and 106).
+    // with CTAs of 256, 412 with 512; of 100 KB: 165 and 200, 184 with 128; of 128 KB: 108 and 106; of 40 KB: 92 and 81 with 128).
     if (a.parts > 1 || (FWD && BWD && (size_t)a.n * sizeof(T) > 120 * 1024)) return distill_rows<T, 512, HARD, FWD, BWD>(a, st);
+    if (a.rows >= kManyRows * sm_count() && (!BWD || (size_t)a.n * sizeof(T) <= 64 * 1024)) return distill_rows<T, 128, HARD, FWD, BWD>(a, st);
     return distill_rows<T, 256, HARD, FWD, BWD>(a, st);
 }
 template <typename T, bool FWD, bool BWD>
