@@ -1,5 +1,7 @@
-"""ctypes binding of libhpf.so: same names as the C ABI, argument marshalling only."""
+"""Binding of libhpf.so: same names as the C ABI, argument marshalling only (ctypes; csrc/py_calls.c where a call is short)."""
 import ctypes as C
+import importlib.machinery
+import importlib.util
 import os
 
 from . import build as _build
@@ -151,23 +153,31 @@ def _dtype_of(dtype, what):
     return d
 
 
-def _ptrs(stream, *named):
-    """Device pointers of (name, tensor or None, torch dtype) and the stream's handle.  A tensor of another type, on the host or on
-    another device than the current one is refused: the kernel would read it wrongly or not at all."""
-    import torch
-    device = torch.cuda.current_device()
-    out = []
-    for name, t, dtype in named:
-        if t is None:
-            out.append(None)
-            continue
-        if t.dtype != dtype:
-            raise HpfError(ERR_INVALID, f"{name}: {dtype} is wanted, got {t.dtype}")
-        if t.get_device() != device:
-            raise HpfError(ERR_INVALID, f"{name} is on {t.device}, the current device is cuda:{device}")
-        out.append(t.data_ptr())
-    out.append(torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
-    return out
+_calls = None
+_CALLS = ("linear_fwd", "linear_bwd", "logprobs_fwd", "logprobs_bwd", "distill_fwd", "distill_bwd", "distill_fwd_bwd")
+
+
+def _refused(status, what, tensor):
+    if what:
+        raise HpfError(status, f"{what}: got {tensor.dtype} on {tensor.device}; tensors are fp32, bf16 or fp16, all of a call's of one type (labels and lists "
+                               "of classes int32, statistics fp32, scratch uint8), on the current device")
+    _check(status)
+
+
+def _fast():
+    """The calls of py_calls.c, with the library's addresses and torch's types."""
+    global _calls
+    if _calls is None:
+        import torch
+        L = lib()
+        loader = importlib.machinery.ExtensionFileLoader("_calls", _build.CALLS)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
+        loader.exec_module(m)
+        torch.cuda.init()
+        m.setup(_refused, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, (torch.float32, torch.bfloat16, torch.float16, torch.int32, torch.uint8),
+                tuple(C.cast(getattr(L, "hpf_" + n), _vp).value for n in _CALLS))
+        _calls = m
+    return _calls
 
 
 def _op_array(ops):
@@ -415,21 +425,12 @@ def linear_scratch_bytes(rows, n_in, n_out, ld_x, ld_y, dtype, act=ACT_NONE, ali
 
 def linear_fwd(x, w, bias, residual, y, z, rows, n_in, n_out, ld_x, ld_y, act, scratch, stream=None):
     """y = act(x W^T + bias) + residual; bias, residual and z (what the activation is applied to) may be None (see hpf.h)."""
-    import torch
-    t = x.dtype
-    dt = _dtype_of(t, "x")
-    *p, ws, st = _ptrs(stream, ("x", x, t), ("w", w, t), ("bias", bias, t), ("residual", residual, t), ("y", y, t), ("z", z, t), ("scratch", scratch, torch.uint8))
-    _check(lib().hpf_linear_fwd(*p, rows, n_in, n_out, ld_x, ld_y, dt, act, ws, scratch.numel(), st))
+    (_calls or _fast()).linear_fwd(x, w, bias, residual, y, z, rows, n_in, n_out, ld_x, ld_y, act, scratch, stream)
 
 
 def linear_bwd(dy, z, x, w, dx, dw, dbias, rows, n_in, n_out, ld_x, ld_y, act, scratch, stream=None):
     """Gradients of linear_fwd, each None if not wanted; dw and dbias may be fp32 whatever the rest is."""
-    import torch
-    t = dy.dtype
-    dt = _dtype_of(t, "dy")
-    g = dw.dtype if dw is not None else dbias.dtype if dbias is not None else t
-    *p, ws, st = _ptrs(stream, ("dy", dy, t), ("z", z, t), ("x", x, t), ("w", w, t), ("dx", dx, t), ("dw", dw, g), ("dbias", dbias, g), ("scratch", scratch, torch.uint8))
-    _check(lib().hpf_linear_bwd(*p, rows, n_in, n_out, ld_x, ld_y, dt, act, _dtype_of(g, "dw"), ws, scratch.numel(), st))
+    (_calls or _fast()).linear_bwd(dy, z, x, w, dx, dw, dbias, rows, n_in, n_out, ld_x, ld_y, act, scratch, stream)
 
 
 def linear_status(scratch):
@@ -440,49 +441,24 @@ def linear_status(scratch):
 # ---- label log-probabilities and distillation: logits [rows][classes] in fp32, bf16 or fp16, rows `ld` elements apart --------
 def logprobs_fwd(logits, labels, logprob, entropy, lse, top_ids, top_logprobs, rows, classes, ld, k=0, temperature=1.0, stream=None):
     """Log-probability of each row's label, entropy, log-sum-exp and the k likeliest classes (see hpf.h); outputs may be None."""
-    import torch
-    f, i = torch.float32, torch.int32
-    dt = _dtype_of(logits.dtype, "logits")
-    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("logprob", logprob, f), ("entropy", entropy, f),
-                   ("lse", lse, f), ("top_ids", top_ids, i), ("top_logprobs", top_logprobs, f))
-    _check(lib().hpf_logprobs_fwd(*p, rows, classes, ld, k, temperature, dt, st))
+    (_calls or _fast()).logprobs_fwd(logits, labels, logprob, entropy, lse, top_ids, top_logprobs, rows, classes, ld, k, temperature, stream)
 
 
 def logprobs_bwd(logits, labels, lse, entropy, d_logprob, d_entropy, d_logits, rows, classes, ld, ld_d, temperature=1.0, stream=None):
     """Gradient of log-probability and entropy; d_logits may be logits."""
-    import torch
-    f = torch.float32
-    dt = _dtype_of(logits.dtype, "logits")
-    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, torch.int32), ("lse", lse, f), ("entropy", entropy, f),
-                   ("d_logprob", d_logprob, f), ("d_entropy", d_entropy, f), ("d_logits", d_logits, logits.dtype))
-    _check(lib().hpf_logprobs_bwd(*p, rows, classes, ld, ld_d, temperature, dt, st))
+    (_calls or _fast()).logprobs_bwd(logits, labels, lse, entropy, d_logprob, d_entropy, d_logits, rows, classes, ld, ld_d, temperature, stream)
 
 
 def distill_fwd(logits, labels, teacher_ids, teacher_logits, loss, stats, rows, classes, ld, k, temperature=1.0, alpha=1.0, stream=None):
     """Loss per row against a teacher's k listed logits, mixed with cross-entropy on the labels (see hpf.h)."""
-    import torch
-    f, i = torch.float32, torch.int32
-    dt = _dtype_of(logits.dtype, "logits")
-    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("teacher_ids", teacher_ids, i),
-                   ("teacher_logits", teacher_logits, f), ("loss", loss, f), ("stats", stats, f))
-    _check(lib().hpf_distill_fwd(*p, rows, classes, ld, k, temperature, alpha, dt, st))
+    (_calls or _fast()).distill_fwd(logits, labels, teacher_ids, teacher_logits, loss, stats, rows, classes, ld, k, temperature, alpha, stream)
 
 
 def distill_bwd(logits, labels, teacher_ids, teacher_logits, stats, d_loss, d_logits, rows, classes, ld, ld_d, k, temperature=1.0, alpha=1.0, stream=None):
     """Its gradient from the statistics that distill_fwd left; d_logits may be logits."""
-    import torch
-    f, i = torch.float32, torch.int32
-    dt = _dtype_of(logits.dtype, "logits")
-    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("teacher_ids", teacher_ids, i),
-                   ("teacher_logits", teacher_logits, f), ("stats", stats, f), ("d_loss", d_loss, f), ("d_logits", d_logits, logits.dtype))
-    _check(lib().hpf_distill_bwd(*p, rows, classes, ld, ld_d, k, temperature, alpha, dt, st))
+    (_calls or _fast()).distill_bwd(logits, labels, teacher_ids, teacher_logits, stats, d_loss, d_logits, rows, classes, ld, ld_d, k, temperature, alpha, stream)
 
 
 def distill_fwd_bwd(logits, labels, teacher_ids, teacher_logits, d_loss, loss, d_logits, rows, classes, ld, ld_d, k, temperature=1.0, alpha=1.0, stream=None):
     """Loss and gradient in one kernel."""
-    import torch
-    f, i = torch.float32, torch.int32
-    dt = _dtype_of(logits.dtype, "logits")
-    *p, st = _ptrs(stream, ("logits", logits, logits.dtype), ("labels", labels, i), ("teacher_ids", teacher_ids, i),
-                   ("teacher_logits", teacher_logits, f), ("d_loss", d_loss, f), ("loss", loss, f), ("d_logits", d_logits, logits.dtype))
-    _check(lib().hpf_distill_fwd_bwd(*p, rows, classes, ld, ld_d, k, temperature, alpha, dt, st))
+    (_calls or _fast()).distill_fwd_bwd(logits, labels, teacher_ids, teacher_logits, d_loss, loss, d_logits, rows, classes, ld, ld_d, k, temperature, alpha, stream)

@@ -1,12 +1,14 @@
-"""Build libhpf.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Build libhpf.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _calls.so (argument marshalling for Python) with the C compiler."""
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhpf.so")
-SOURCES = ["hpf_model.cu", "kernels_mem.cu", "conv_simt.cu", "conv_tc.cu", "conv_pipe.cu", "no_alloc.cu", "bn_resident.cu", "logits.cu", "linear.cu"]
+CALLS = os.path.join(HERE, "_calls.so")
+SOURCES = ["hpf_model.cu", "kernels_mem.cu", "conv_simt.cu", "conv_tc.cu", "conv_pipe.cu", "no_alloc.cu", "bn_resident.cu", "logprobs.cu", "distill.cu", "linear.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "--use_fast_math=false"]
 
@@ -16,9 +18,9 @@ def _sources():
 
 
 def _stale():
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "hpf.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -43,6 +45,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
             raise RuntimeError("nvcc failed: " + " ".join(cmd))
     link = [nvcc, "-shared", "-o", LIB] + objs + ["-lcudart"]
     subprocess.run(link, check=True)
+    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "py_calls.c"), "-o", CALLS],
+                   check=True)
     return LIB
 
 
