@@ -274,28 +274,12 @@ __device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank)
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
     return there;
 }
-// The same towards the CTAs of a cluster.  A tile's quarter blocks (8 rows x 32 columns, 1 KB) are dealt out to the ranks; the owner
-// keeps the `split` versions of a quarter side by side.  Stores to another CTA need no answer: reading the partial tiles over from their
-// owners instead left a warp waiting 5 us for a 128 x 128 tile of four.
-__device__ __forceinline__ void block_push(uint32_t slots, int block, int lane, const float* v, int swap, int split, int rank, int rows)
+// Towards the CTAs of a cluster: a tile's quarter blocks (8 rows x 32 columns, 1 KB) are dealt out to the ranks; the owner gets the `split`
+// versions of a quarter side by side, by bulk copies that its barrier counts.  (Stores to the owners took 3.6 us for a 128 x 128 tile of four,
+// loads from the others 5.)
+__device__ __forceinline__ void send_quarter(uint32_t src, uint32_t dst, uint32_t bar)
 {
-    if (!swap) {
-        const int i = block * 4 + (lane >> 3);
-        const uint32_t to = at_rank(slots + ((i & -split) + rank) * 1024, i & (split - 1));
-        if (lane < rows) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(unit_at(to, lane & 7, u)), "f"(v[4 * u]), "f"(v[4 * u + 1]), "f"(v[4 * u + 2]), "f"(v[4 * u + 3])
-                             : "memory");
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const int i = block * 4 + (j >> 3);
-            const uint32_t to = at_rank(slots + ((i & -split) + rank) * 1024, i & (split - 1));
-            if (j < rows) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(unit_at(to, j & 7, lane >> 2) + (lane & 3) * 4), "f"(v[j]) : "memory");
-        }
-    }
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], 1024, [%2];" ::"r"(dst), "r"(src), "r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src, int c0, int c1)
@@ -418,10 +402,8 @@ __device__ __forceinline__ void send_block(const GemmArgs& p, uint32_t slabs, ui
     else store_slab<T>(p.out, p, slabs, v, row0, col0, lane);
 }
 
-__device__ __forceinline__ void cluster_barrier()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // One warp finishes ROWS_IN rows of out from (row0, col0) on, 32 columns wide, whose fp32 sums lie in shared memory: bias, activation,
 // residual, one rounding.  `split` versions of the sums, 1 KB apart, are added up in order.  16 bytes of a row per lane where rows lie on
@@ -549,12 +531,12 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
     using S = Shape<E, BN>;
     constexpr int STAGES = S::kStages;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) unsigned long long s_bars[3 * kMaxStages + 4];
+    __shared__ __align__(8) unsigned long long s_bars[3 * kMaxStages + 5];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t staging = ring + kRing;
-    const uint32_t full = smem_u32(s_bars), empty = full + 8 * kMaxStages, ready = empty + 8 * kMaxStages, acc_full = ready + 8 * kMaxStages, acc_empty = acc_full + 16;
+    const uint32_t full = smem_u32(s_bars), empty = full + 8 * kMaxStages, ready = empty + 8 * kMaxStages, acc_full = ready + 8 * kMaxStages, acc_empty = acc_full + 16, joined = acc_empty + 16;
     const int warp = warp_index(), lane = threadIdx.x & 31;
     const int split = p.split;
     const int rank = split > 1 ? (int)(blockIdx.x % (unsigned)split) : 0;
@@ -573,6 +555,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
             mbar_init(empty + 8 * i, 1);
             mbar_init(ready + 8 * i, 4);
         }
+        mbar_init(joined, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(acc_full + 8 * i, 1);
             mbar_init(acc_empty + 8 * i, kOutWarps);
@@ -747,28 +730,49 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
         }
         if (p.copy_out && lane == 0) tma_store_wait<0>();
         if (split > 1) {
-            cluster_barrier();                                 // every product of the cluster is done: the rings are free
-            if (live && (BN > 32 || half == 0)) {
-                const Tile tile = tile_at(first, p.tiles_m, p.tiles_n);
+            const Tile tile = tile_at(first, p.tiles_m, p.tiles_n);
+            const uint32_t slots = ring + kRing / 2;           // versions of the quarters that this CTA adds up
+            const bool mine_too = live && (BN > 32 || half == 0);
+            // the first row of out of quarter i of the tile
+            const auto row_of = [&](int i) { return (p.swap ? tile.n * BN + (i >> 4) * 32 : tile.m * kTileM + ((i >> 2) & 3) * 32) + (i & 3) * 8; };
+            if (mine_too) {
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) {
-                    const int c = half * BLOCKS + b, at_m = tile.m * kTileM + quad * 32, at_n = tile.n * BN + c * 32;
+                    const int c = half * BLOCKS + b;
                     float v[32];
                     if constexpr (!PROMOTE) tmem_ld32(tmem + lanes + c * 32, v);
                     const float* sums = v;
                     if constexpr (PROMOTE) sums = acc[b];
-                    block_push(ring, c * 4 + quad, lane, sums, p.swap, split, rank, p.rows - (p.swap ? at_n : at_m));
+                    block_put(ring + (c * 4 + quad) * kBlock, lane, sums, p.swap);
                 }
+                fence_async_smem();
             }
-            cluster_barrier();
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();                                    // every product of the cluster is done: the rings are free
+            if (warp == 4 && lane == 0) {
+                int expected = 0;
+                for (int i = rank; i < BN / 32 * 16; i += split) expected += row_of(i) < p.rows;
+                mbar_expect_tx(joined, (uint32_t)(expected * split * 1024));
+            }
+            if (mine_too && lane < 4 * BLOCKS) {
+                const int i = ((half * BLOCKS + (lane >> 2)) * 4 + quad) * 4 + (lane & 3), owner = i & (split - 1);
+                if (row_of(i) < p.rows) send_quarter(ring + i * 1024, at_rank(slots + ((i & -split) + rank) * 1024, owner), at_rank(joined, owner));
+            }
+            __syncwarp();
+            live = mbar_wait(joined, 0, abort_flag) && live;
+            live = __all_sync(0xffffffffu, live);
+            if (!live) report(p.status, 45);
+            cluster_arrive();                                  // what was sent to this CTA has left its senders
             if (live) {
-                const Tile tile = tile_at(first, p.tiles_m, p.tiles_n);
                 for (int i = warp - 4; i * split + rank < BN / 32 * 16; i += kOutWarps) {
-                    const int item = i * split + rank, u = item >> 2;
-                    const int at_m = tile.m * kTileM + (u & 3) * 32, at_n = tile.n * BN + (u >> 2) * 32;
-                    finish_rows<T, 8>(p, ring + i * split * 1024, split, (p.swap ? at_n : at_m) + (item & 3) * 8, p.swap ? at_m : at_n, lane);
+                    const int item = i * split + rank;
+                    const int col0 = p.swap ? tile.m * kTileM + ((item >> 2) & 3) * 32 : tile.n * BN + (item >> 4) * 32;
+                    finish_rows<T, 8>(p, slots + i * split * 1024, split, row_of(item), col0, lane);
                 }
             }
+            __syncwarp();
+            cluster_wait();
         }
     } else if (E == 4 && warp >= 4 + kOutWarps) {
         // lo parts: what a TF32 operand drops of each value, beside the stage, in the same places
@@ -805,8 +809,10 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
 
     if (split > 1 && !(warp >= 4 && warp < 4 + kOutWarps)) {
         __syncwarp();
-        cluster_barrier();
-        cluster_barrier();
+        cluster_arrive();
+        cluster_wait();
+        cluster_arrive();
+        cluster_wait();
     }
     tc_fence_before();
     __syncthreads();
@@ -928,14 +934,34 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ 
     if (p.parts > 1) cg::this_cluster().sync();
 }
 
-// Rows that a tensor copy cannot address (start or stride off 16 bytes), laid out again at a stride that it can.
+// Rows that a tensor copy cannot address (start or stride off 16 bytes), laid out again at a stride that it can: 16 bytes a thread, `across`
+// threads along a row.
 template <typename T>
-__global__ void __launch_bounds__(256) linear_repack_kernel(const T* in, T* out, int64_t rows, int n, int64_t ld, int64_t ld_out)
+__global__ void __launch_bounds__(256) linear_repack_kernel(const T* in, T* out, int64_t rows, int n, int64_t ld, int64_t ld_out, int across)
 {
+    constexpr int V = 16 / (int)sizeof(T);
+    const int col = (int)(blockIdx.x * across + threadIdx.x % across) * V, down = 256 / across;
     pdl_launch_dependents();
     pdl_wait();
-    for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (int64_t)gridDim.x * 8)
-        for (int c = threadIdx.x & 31; c < n; c += 32) out[r * ld_out + c] = in[r * ld + c];
+    if (col >= n) return;
+    const int64_t step = (int64_t)gridDim.y * down;
+#pragma unroll 4
+    for (int64_t r = (int64_t)blockIdx.y * down + threadIdx.x / across; r < rows; r += step) {
+        const T* at = in + r * ld + col;
+        uint4 v;
+        // pieces reach up to 15 bytes to either side: never out of the first row's start nor of the last row's end
+        if (col + V <= n && !(r == 0 && col < V) && !(r == rows - 1 && col + 2 * V > n)) {
+            Piece<true> p;
+            p.load(reinterpret_cast<const char*>(at));
+            v = p.get(reinterpret_cast<const char*>(at));
+        } else {
+            T w[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) w[j] = col + j < n ? at[j] : T(0);
+            memcpy(&v, w, 16);
+        }
+        *reinterpret_cast<uint4*>(out + r * ld_out + col) = v;
+    }
 }
 
 // ---- host side ----------------------------------------------------------------------------------------------------------
@@ -956,10 +982,10 @@ int sm_count()
 // itself up, and waits for the predecessor's results before its first access to global memory.  (A backward pass is three kernels, 2 us of
 // launch and set-up each otherwise.)
 template <typename... KArgs, typename... Args>
-cudaError_t launch(void (*kernel)(KArgs...), unsigned grid, int threads, size_t smem, int cluster, cudaStream_t st, const Args&... args)
+cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, const Args&... args)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -1065,7 +1091,7 @@ Plan choose(int64_t lanes, int64_t cols, int k_blocks, int narrowest, int widest
         const double products = mmas * (bn == 256 ? 128.0 : bn == 128 ? 64.0 : bn == 64 ? 48.0 : 39.0), copies = (kTileM + bn) * kRow / 48.0;
         const double stage = products > copies ? products : copies;
         for (int i = 0, split = 1; split <= kMaxSplit; ++i, split *= 2) {
-            if (split > 1 && (k_blocks < 2 * split || tiles > 2 * fit.clusters[i])) break;
+            if (split > 1 && (bn == 256 || k_blocks < 2 * split || tiles > 2 * fit.clusters[i])) break;      // (two versions of 256 columns do not fit the ring)
             const int64_t waves = (tiles + fit.clusters[i] - 1) / fit.clusters[i];
             const double t = waves * (((k_blocks + split - 1) / split) * stage + 6.0 * bn) + 2500.0 + (split > 1 ? 1500.0 : 0.0);
             if (t < least) { least = t; best = Plan{bn, split}; }
@@ -1137,10 +1163,15 @@ cudaError_t gemm_any(GemmArgs& g, const Operand& a, const Operand& b, int64_t ro
 
 cudaError_t repack(const void* in, void* out, int64_t rows, int n, int64_t ld, int64_t ld_out, int e, cudaStream_t st)
 {
-    const int64_t blocks = (rows + 7) / 8;
-    const unsigned grid = (unsigned)(blocks < 8 * sm_count() ? blocks : 8 * sm_count());
-    if (e == 4) return launch(linear_repack_kernel<uint32_t>, grid, 256, 0, 1, st, static_cast<const uint32_t*>(in), static_cast<uint32_t*>(out), rows, n, ld, ld_out);
-    return launch(linear_repack_kernel<uint16_t>, grid, 256, 0, 1, st, static_cast<const uint16_t*>(in), static_cast<uint16_t*>(out), rows, n, ld, ld_out);
+    const int pieces = (int)(((int64_t)n * e + 15) / 16);
+    int across = 256;
+    while (across > 8 && across / 2 >= pieces) across /= 2;
+    const int64_t wide = (pieces + across - 1) / across, high = (rows + 256 / across - 1) / (256 / across);
+    // (a few rows a thread where there are more than the GPU holds at a time)
+    const int64_t most = (16 * sm_count() + wide - 1) / wide;
+    const dim3 grid((unsigned)wide, (unsigned)(high < most ? high : most < 65535 ? most : 65535));
+    if (e == 4) return launch(linear_repack_kernel<uint32_t>, grid, 256, 0, 1, st, static_cast<const uint32_t*>(in), static_cast<uint32_t*>(out), rows, n, ld, ld_out, across);
+    return launch(linear_repack_kernel<uint16_t>, grid, 256, 0, 1, st, static_cast<const uint16_t*>(in), static_cast<uint16_t*>(out), rows, n, ld, ld_out, across);
 }
 
 template <typename T>
