@@ -19,6 +19,7 @@
 #include "../../include/hpf.h"
 #include "conv_tc.h"
 #include "hpf_kernels.h"
+#include "pairs.cuh"
 #include "tc_ptx.cuh"
 
 #include <cooperative_groups.h>
@@ -162,47 +163,61 @@ template <> struct Pack<__half> {
     static __device__ __forceinline__ __half put(float v) { return __float2half_rn(v); }
 };
 
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ float reciprocal(float x)
 {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ f2 both(float v) { return pair(v, v); }
 // gelu is z Phi(z), its slope Phi(z) + z phi(z).  Phi by Abramowitz and Stegun 7.1.26: with x = |z| / sqrt 2 and t = 1 / (1 + p x),
 // 1 - erf x = (a1 t + ... + a5 t^5) e^(-x^2) within 1.5e-7, and e^(-x^2) = e^(-z^2 / 2) is what phi needs too: 2 special-function
 // results a value where erff and expf took about 60 instructions (the dz kernel of 8192 x 16384 bf16: 354 us with those).
-__device__ __forceinline__ void gauss(float z, float* cdf, float* bell)
+// Gives Phi and e^(-z^2 / 2).
+__device__ __forceinline__ void gauss(f2 z, f2* cdf, f2* e)
 {
-    const float x = fabsf(z) * 0.70710678118f;
-    const float t = reciprocal(fmaf(0.3275911f, x, 1.f));
-    const float e = ex2(z * z * -0.72134752044f);
-    const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    *cdf = z > 0.f ? 1.f - tail : tail;
-    *bell = e * 0.39894228040f;
+    float z0, z1, d0, d1;
+    split(z, &z0, &z1);
+    split(fma2(pair(fabsf(z0), fabsf(z1)), both(0.3275911f * 0.70710678118f), both(1.f)), &d0, &d1);
+    const f2 t = pair(reciprocal(d0), reciprocal(d1));
+    *e = ex2_2(mul2(mul2(z, z), both(-0.72134752044f)));
+    f2 q = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+    q = fma2(t, q, both(0.5f * 1.421413741f));
+    q = fma2(t, q, both(0.5f * -0.284496736f));
+    q = fma2(t, q, both(0.5f * 0.254829592f));
+    const f2 tail = mul2(mul2(t, q), *e);
+    float t0, t1, u0, u1;
+    split(tail, &t0, &t1);
+    split(fma2(tail, both(-1.f), both(1.f)), &u0, &u1);
+    *cdf = pair(z0 > 0.f ? u0 : t0, z1 > 0.f ? u1 : t1);
 }
-__device__ __forceinline__ float sigmoid(float z) { return reciprocal(1.f + ex2(z * -1.44269504089f)); }
+__device__ __forceinline__ f2 sigmoid(f2 z)
+{
+    float a, b;
+    split(add2(ex2_2(mul2(z, both(-1.44269504089f))), both(1.f)), &a, &b);
+    return pair(reciprocal(a), reciprocal(b));
+}
 template <int V>
 __device__ __forceinline__ void activate(float* v, int act)
 {
+    static_assert(V % 2 == 0, "values in pairs");
     if (act == HPF_ACT_RELU) {
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = v[j] < 0.f ? 0.f : v[j];          // a NaN stays
     } else if (act == HPF_ACT_GELU) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float cdf, bell;
-            gauss(v[j], &cdf, &bell);
-            v[j] *= cdf;
+        for (int j = 0; j < V; j += 2) {
+            const f2 z = pair(v[j], v[j + 1]);
+            f2 cdf, e;
+            gauss(z, &cdf, &e);
+            split(mul2(z, cdf), &v[j], &v[j + 1]);
         }
     } else if (act == HPF_ACT_SILU) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] *= sigmoid(v[j]);
+        for (int j = 0; j < V; j += 2) {
+            const f2 z = pair(v[j], v[j + 1]);
+            split(mul2(z, sigmoid(z)), &v[j], &v[j + 1]);
+        }
     }
 }
 // g *= act'(z)
@@ -212,19 +227,21 @@ __device__ __forceinline__ void apply_slope(float* g, const float* z, int act)
     if (act == HPF_ACT_RELU) {
 #pragma unroll
         for (int j = 0; j < V; ++j) g[j] = z[j] > 0.f ? g[j] : z[j] != z[j] ? z[j] : 0.f;
-    } else if (act == HPF_ACT_GELU) {
+        return;
+    }
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float cdf, bell;
-            gauss(z[j], &cdf, &bell);
-            g[j] *= fmaf(z[j], bell, cdf);
+    for (int j = 0; j < V; j += 2) {
+        const f2 zz = pair(z[j], z[j + 1]);
+        f2 s;
+        if (act == HPF_ACT_GELU) {
+            f2 e;
+            gauss(zz, &s, &e);
+            s = fma2(mul2(zz, both(0.39894228040f)), e, s);
+        } else {
+            s = sigmoid(zz);                                                 // s (1 + z (1 - s))
+            s = mul2(s, fma2(zz, fma2(s, both(-1.f), both(1.f)), both(1.f)));
         }
-    } else if (act == HPF_ACT_SILU) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float s = sigmoid(z[j]);
-            g[j] *= s * fmaf(z[j], 1.f - s, 1.f);
-        }
+        split(mul2(pair(g[j], g[j + 1]), s), &g[j], &g[j + 1]);
     }
 }
 
@@ -854,10 +871,10 @@ struct Piece {
 
 // A CTA goes down 128 bytes of columns, 32 rows at a time; `parts` CTAs of a cluster share the rows and add their sums up in rank order.
 // The loads of U rows a thread are issued before the first is used.
-template <typename T, bool SHIFT>
-__global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ DzArgs p)
+template <typename T, bool SHIFT, bool ACT>
+__global__ void __launch_bounds__(256, SHIFT ? 3 : 4) linear_dz_kernel(const __grid_constant__ DzArgs p)
 {
-    constexpr int COLS = 128 / sizeof(T), V = Pack<T>::V, ROWS = 32, U = SHIFT ? 2 : 4;
+    constexpr int COLS = 128 / sizeof(T), V = Pack<T>::V, ROWS = 32, U = ACT || SHIFT ? 2 : 4;
     __shared__ float s_sum[8][COLS];
     __shared__ float s_total[COLS];
     const int part = (int)(blockIdx.x % (unsigned)p.parts);
@@ -869,46 +886,53 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const __grid_constant__ 
     for (int j = 0; j < V; ++j) sum[j] = 0.f;
     const T *dy = reinterpret_cast<const T*>(p.dy) + c0 + col, *z = reinterpret_cast<const T*>(p.z) + c0 + col;
     T* dz = reinterpret_cast<T*>(p.dz) + c0 + col;
-    const bool act = p.act != HPF_ACT_NONE;
-    const int64_t step = (int64_t)p.parts * ROWS;
+    const int step = p.parts * ROWS;
     const int there = p.n - c0 - col;                        // columns from here on
     pdl_launch_dependents();
     pdl_wait();
-    for (int64_t r0 = (int64_t)part * ROWS + (threadIdx.x >> 3); r0 < p.rows; r0 += U * step) {
-        Piece<SHIFT> gp[U], zp[U];
-        bool whole[U];
+    const int64_t first = (int64_t)part * ROWS + (threadIdx.x >> 3);
+    dy += first * p.ld;
+    z += first * p.ld;
+    dz += first * p.ld_dz;
+    for (int64_t r0 = first; r0 < p.rows; r0 += U * step) {
+        Piece<SHIFT> gp[U], zp[ACT ? U : 1];
+        uint32_t whole = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             // a shifted piece reaches up to 15 bytes to either side: never out of the first row's start nor of the last row's end
             const int64_t r = r0 + u * step;
-            whole[u] = r < p.rows && there >= V;
-            if (SHIFT && ((r == 0 && c0 + col < V) || (r == p.rows - 1 && there < 2 * V))) whole[u] = false;
-            if (whole[u]) {
-                gp[u].load(reinterpret_cast<const char*>(dy + r * p.ld));
-                if (act) zp[u].load(reinterpret_cast<const char*>(z + r * p.ld));
+            bool in = r < p.rows && there >= V;
+            if (SHIFT && ((r == 0 && c0 + col < V) || (r == p.rows - 1 && there < 2 * V))) in = false;
+            if (in) {
+                whole |= 1u << u;
+                gp[u].load(reinterpret_cast<const char*>(dy + u * step * p.ld));
+                if (ACT) zp[ACT ? u : 0].load(reinterpret_cast<const char*>(z + u * step * p.ld));
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t r = r0 + u * step;
-            if (r >= p.rows) break;
+            if (r0 + u * step >= p.rows) break;
+            const T *g_at = dy + u * step * p.ld, *z_at = z + u * step * p.ld;
             float g[V], zv[V];
-            if (whole[u]) {
-                Pack<T>::unpack(gp[u].get(reinterpret_cast<const char*>(dy + r * p.ld)), g);
-                if (act) Pack<T>::unpack(zp[u].get(reinterpret_cast<const char*>(z + r * p.ld)), zv);
+            if (whole >> u & 1) {
+                Pack<T>::unpack(gp[u].get(reinterpret_cast<const char*>(g_at)), g);
+                if (ACT) Pack<T>::unpack(zp[ACT ? u : 0].get(reinterpret_cast<const char*>(z_at)), zv);
             } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    g[j] = j < there ? Pack<T>::get(dy[r * p.ld + j]) : 0.f;
-                    zv[j] = j < there && act ? Pack<T>::get(z[r * p.ld + j]) : 0.f;
+                    g[j] = j < there ? Pack<T>::get(g_at[j]) : 0.f;
+                    zv[j] = ACT && j < there ? Pack<T>::get(z_at[j]) : 0.f;
                 }
             }
-            if (act) apply_slope<V>(g, zv, p.act);
+            if (ACT) apply_slope<V>(g, zv, p.act);
 #pragma unroll
             for (int j = 0; j < V; ++j) sum[j] += g[j];
             // dz is rounded to the operands' type: the tensor cores take it in that type only.  Its rows are whole numbers of 128 bytes long.
-            if (p.dz && there > 0) *reinterpret_cast<uint4*>(dz + r * p.ld_dz) = Pack<T>::pack(g);
+            if (p.dz && there > 0) *reinterpret_cast<uint4*>(dz + u * step * p.ld_dz) = Pack<T>::pack(g);
         }
+        dy += U * step * p.ld;
+        z += U * step * p.ld;
+        dz += U * step * p.ld_dz;
     }
     if (!p.db) return;
 #pragma unroll
@@ -1182,7 +1206,8 @@ cudaError_t launch_dz(DzArgs& a, cudaStream_t st)
     const int64_t want = (a.rows + 255) / 256;
     a.parts = (int)(want > 8 ? 8 : want);
     const bool wide = aligned16(a.dy) && (a.ld * sizeof(T)) % 16 == 0 && (a.act == HPF_ACT_NONE || aligned16(a.z));
-    auto* kernel = wide ? linear_dz_kernel<T, false> : linear_dz_kernel<T, true>;
+    auto* kernel = a.act == HPF_ACT_NONE ? (wide ? linear_dz_kernel<T, false, false> : linear_dz_kernel<T, true, false>)
+                                         : (wide ? linear_dz_kernel<T, false, true> : linear_dz_kernel<T, true, true>);
     return launch(kernel, (unsigned)((a.n + cols - 1) / cols * a.parts), 256, 0, a.parts, st, a);
 }
 

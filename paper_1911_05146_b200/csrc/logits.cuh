@@ -13,6 +13,7 @@
 #pragma once
 #include "../../include/hpf.h"
 #include "hpf_kernels.h"
+#include "pairs.cuh"
 
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -31,13 +32,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFloor = -1e30f;   // stands for -inf where it meets a weight of 0
 
 __device__ __forceinline__ float ninf() { return __int_as_float(0xff800000); }
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // ---- element types ---------------------------------------------------------------------------------------------------
 template <typename T> struct Io;
 template <> struct Io<float> {
@@ -177,20 +171,6 @@ struct Share {
 };
 
 // ---- running sums ----------------------------------------------------------------------------------------------------
-// Two values in one instruction: the loops below are bound by what an SM issues, not by its arithmetic.
-typedef unsigned long long f2;
-__device__ __forceinline__ f2 pair(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ void split(f2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
-__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ f2 ex2_2(f2 v)
-{
-    float a, b;
-    split(v, &a, &b);
-    return pair(ex2(a), ex2(b));
-}
-
 // m: largest logit, s = sum 2^((v - m) c), w = sum 2^((v - m) c) (v - m), h = the sum of s at temperature 1
 struct Sums {
     float m, s, w, h;

@@ -8,6 +8,7 @@ namespace {
 constexpr int kMaxTop = 64;        // classes listed per row
 constexpr int kGroups = 128;       // groups of threads whose maxima bound the k-th largest class
 constexpr int kCandidates = 512;   // classes at or above that bound that are ranked by counting
+constexpr int kWarpCandidates = 192;
 
 // The upper half of a logit's place among the floats: in their order, equal where the upper 16 bits are.
 __device__ __forceinline__ uint32_t order16(float v)
@@ -76,14 +77,10 @@ __device__ __forceinline__ void over_stretches(const Share<T>& sh, const TopShar
     }
 }
 
-// One warp: the k-th largest of the maxima of 32 groups of threads (a lane's group: threads lane, lane + 32, ...), by a bitonic sort.
+// One warp: the k-th largest of its lanes' values, by a bitonic sort; of the maxima of 32 groups of threads (a lane's: lane, lane + 32, ...).
 constexpr int kFewTop = 16;
-template <int NT>
-__device__ __forceinline__ float kth_of_32(const float* maxima, int k, int lane)
+__device__ __forceinline__ float kth_of_warp(float v, int k, int lane)
 {
-    float v = ninf();
-#pragma unroll
-    for (int t = 0; t < NT; t += 32) v = fmaxf(v, maxima[t + lane]);
 #pragma unroll
     for (int size = 2; size <= 32; size *= 2)
 #pragma unroll
@@ -94,18 +91,20 @@ __device__ __forceinline__ float kth_of_32(const float* maxima, int k, int lane)
         }
     return __shfl_sync(0xffffffffu, v, k - 1);
 }
-// The same of 128 groups (threads t, t + 128, ...), to the upper 16 bits: four keys a lane, the bound found bit by bit.
 template <int NT>
-__device__ __forceinline__ float kth_of_128(const float* maxima, int k, int lane)
+__device__ __forceinline__ float kth_of_32(const float* maxima, int k, int lane)
 {
-    uint32_t key[kGroups / 32];
+    float v = ninf();
 #pragma unroll
-    for (int i = 0; i < kGroups / 32; ++i) {
-        float v = ninf();
+    for (int t = 0; t < NT; t += 32) v = fmaxf(v, maxima[t + lane]);
+    return kth_of_warp(v, k, lane);
+}
+// The k-th largest of 128 values, four a lane, to the upper 16 bits: found bit by bit.
+__device__ __forceinline__ float kth_of_four(const float (&value)[4], int k)
+{
+    uint32_t key[4];
 #pragma unroll
-        for (int t = 0; t < NT; t += kGroups) v = fmaxf(v, maxima[t + i * 32 + lane]);
-        key[i] = order16(v);
-    }
+    for (int i = 0; i < 4; ++i) key[i] = order16(value[i]);
     // the bits that all keys share are the bound's too
     const uint32_t most = __reduce_max_sync(0xffffffffu, max(max(key[0], key[1]), max(key[2], key[3])));
     const uint32_t least = __reduce_min_sync(0xffffffffu, min(min(key[0], key[1]), min(key[2], key[3])));
@@ -113,11 +112,26 @@ __device__ __forceinline__ float kth_of_128(const float* maxima, int k, int lane
     for (; bit; bit >>= 1) {
         int count = 0;
 #pragma unroll
-        for (int i = 0; i < kGroups / 32; ++i) count += __popc(__ballot_sync(0xffffffffu, key[i] >= (bound | bit)));
+        for (int i = 0; i < 4; ++i) count += __popc(__ballot_sync(0xffffffffu, key[i] >= (bound | bit)));
         if (count >= k) bound |= bit;
     }
     const uint32_t o = bound << 16;
     return bound ? __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)) : ninf();
+}
+
+// Of 128 groups of threads (t, t + 128, ...).
+template <int NT>
+__device__ __forceinline__ float kth_of_128(const float* maxima, int k, int lane)
+{
+    static_assert(kGroups == 128, "four groups a lane");
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = ninf();
+#pragma unroll
+        for (int t = 0; t < NT; t += kGroups) v[i] = fmaxf(v[i], maxima[t + i * 32 + lane]);
+    }
+    return kth_of_four(v, k);
 }
 
 // The k largest classes of this CTA's share are among the sm.cand[0 .. the result); sm.rank has their places.  Every thread knows the largest logit of each stretch of its strip
@@ -307,7 +321,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprobs_fwd_kernel(const __gri
     }
 }
 
-// A warp per row of at most 32 J classes, all in registers; the list is taken one class at a time.
+// A warp per row of at most 32 J classes, all in registers.
 template <typename T, int J>
 __global__ void __launch_bounds__(128) logprobs_fwd_warp_kernel(const __grid_constant__ LogprobsArgs p)
 {
@@ -332,6 +346,36 @@ __global__ void __launch_bounds__(128) logprobs_fwd_warp_kernel(const __grid_con
     if (lane == 0) write_stats<T>(p, row, a);
     if (p.k == 0) return;
     const float ln_s = logf(a.s);
+    if constexpr (J > 1) {
+        // as in select_top: classes at or above the k-th largest maximum (of the lanes, or of four groups a lane) are candidates, ranked by counting
+        __shared__ unsigned long long s_cand[4][kWarpCandidates];
+        unsigned long long* cand = s_cand[threadIdx.x >> 5];
+        float top[4] = {ninf(), ninf(), ninf(), ninf()};
+#pragma unroll
+        for (int j = 0; j < J; ++j) top[j & 3] = fmaxf(top[j & 3], v[j]);
+        const float bound = p.k <= kFewTop ? kth_of_warp(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), p.k, lane) : kth_of_four(top, p.k);
+        int count = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const bool in = v[j] >= bound && v[j] > ninf();
+            const uint32_t which = __ballot_sync(0xffffffffu, in);
+            const int at = count + __popc(which & ((1u << lane) - 1));
+            if (in && at < kWarpCandidates) cand[at] = class_key(v[j], lane + 32 * j);
+            count += __popc(which);
+        }
+        if (count <= kWarpCandidates) {                       // (long runs of equal logits go on below)
+            __syncwarp();
+            for (int i = lane; i < count; i += 32) {
+                const unsigned long long mine = cand[i];
+                int rank = 0;
+#pragma unroll 8
+                for (int j = 0; j < count; ++j) rank += cand[j] > mine;
+                if (rank < p.k) write_top(p, row, rank, mine, a.m, ln_s);
+            }
+            for (int i = count + lane; i < p.k; i += 32) write_top(p, row, i, 0ull, a.m, ln_s);
+            return;
+        }
+    }
     uint32_t o[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) o[j] = (uint32_t)(class_key(v[j], 0) >> 32);
@@ -461,9 +505,16 @@ __global__ void __launch_bounds__(128) logprobs_bwd_warp_kernel(const __grid_con
     RowScale s{lse / p.inv_t, 1.f, false};
     if (!g.dead && !(fabsf(lse) < kLseExact)) s = scale_of(warp_run_over<T, false>(x, p.n, g.c, lane));
     g.scale(s);
-    for (int i = lane; i < p.n; i += 32) {
-        const float v = Io<T>::get(x[i]);
-        out[i] = Io<T>::put(g.dead ? 0.f : i == g.label ? g.label_value(v) : g.slow(v));
+    for (int i0 = lane; i0 < p.n; i0 += 256) {               // eight loads under way (`out` may be x: they cannot pass the stores)
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i0 + 32 * j < p.n) v[j] = Io<T>::get(x[i0 + 32 * j]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = i0 + 32 * j;
+            if (i < p.n) out[i] = Io<T>::put(g.dead ? 0.f : i == g.label ? g.label_value(v[j]) : g.slow(v[j]));
+        }
     }
 }
 
