@@ -358,15 +358,15 @@ int hpf_sgd_momentum_flat(const float *d_slots, float *d_grad_avg, float *d_para
  * Logits: d_logits [rows][classes] of type dtype, rows `ld` elements apart (any alignment the type has); 16-bit types are
  * computed with in fp32.  A logit of -inf is a masked class: it has probability 0, is never listed and gets gradient 0.
  * A row with nothing but -inf has no distribution (see each call).  A row with a NaN or +inf gives NaN.  A label
- * outside [0, classes) is no label.  Statistics, losses and lists are fp32 / int32.  No workspace; a call is one
- * kernel on `stream` of the current device, may be captured, and rows = 0 does nothing.  Results do not depend on timing. */
+ * outside [0, classes) is no label.  Statistics, losses and lists are fp32 / int32.  No workspace; temperatures lie in
+ * [1e-30, 1e30]; a call is one kernel on `stream` of the current device, may be captured, and rows = 0 does nothing.  Results do not depend on timing. */
 typedef enum { HPF_FP32 = 0, HPF_BF16 = 1, HPF_FP16 = 2 } hpf_dtype;
 
 /* The linear layer  z = x W^T + bias,  y = act(z) + residual:  d_x [rows][n_in] (rows ld_x elements apart), d_w [n_out][n_in],
  * d_bias [n_out] or NULL, d_residual and d_y [rows][n_out] (rows ld_y apart; d_residual may be NULL, or d_y itself), d_z like d_y: where
  * the backward call needs it (any activation but NONE), else NULL.  All of type dtype, sums in fp32; fp32 tensors go through the
  * tensor cores as three TF32 products per term (each within 3 2^-20; an infinity in x or W gives NaN).  GELU is z Phi(z), SILU z / (1 + e^-z).
- * Any sizes, strides and alignments that the type has; rows that do not start on 16-byte boundaries cost a copy in scratch.
+ * No output may overlap an input but as said.  Any sizes, strides and alignments that the type has; rows that do not start on 16-byte boundaries cost a copy in scratch.
  * d_scratch: 16-byte aligned, scratch_bytes of it as hpf_linear_scratch_bytes says (aligned = 0: for tensors whose first element
  * is not on a 16-byte boundary); its first 8 bytes are zeroed once by the caller and tell hpf_linear_status whether a bounded wait ever
  * gave up.  Calls that may overlap need a scratch each.  rows = 0: nothing is written but zero gradients of W and bias. */
@@ -382,7 +382,7 @@ int hpf_linear_fwd(const void *d_x, const void *d_w, const void *d_bias, const v
 int hpf_linear_bwd(const void *d_dy, const void *d_z, const void *d_x, const void *d_w, void *d_dx, void *d_dw, void *d_dbias, int64_t rows,
                    int32_t n_in, int32_t n_out, int64_t ld_x, int64_t ld_y, int32_t dtype, int32_t act, int32_t grad_type,
                    void *d_scratch, size_t scratch_bytes, void *stream);
-/* 1 if a bounded wait of a call on this scratch gave up since its head was zeroed (waits for those calls). */
+/* 1 if a bounded wait of a linear call on this scratch gave up since its head was zeroed (waits for those calls). */
 int hpf_linear_status(const void *d_scratch, int32_t *h_gave_up);
 
 /* With s = logits / temperature:  d_lse = ln sum exp s;  d_logprob = s[label] - lse (0 without a label; -inf for a masked

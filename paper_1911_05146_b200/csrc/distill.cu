@@ -320,7 +320,7 @@ int check_distill(const void* logits, const int32_t* labels, const int32_t* ids,
 {
     const int bad = check_rows(logits, rows, classes, ld, dtype);
     if (bad != HPF_OK) return bad;
-    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature)) return api_fail(HPF_ERR_INVALID, "the temperature must be positive");
+    if (!temperature_ok(temperature)) return api_fail(HPF_ERR_INVALID, "the temperature must lie in [1e-30, 1e30]");
     if (!(alpha >= 0.f && alpha <= 1.f)) return api_fail(HPF_ERR_INVALID, "alpha must lie in [0, 1]");
     if (k < 0 || k > kMaxTeacher) return api_fail(HPF_ERR_UNSUPPORTED, "a teacher's list has at most 256 entries per row");
     if (rows && ((k && (!ids || !teacher)) || (alpha < 1.f && !labels))) return api_fail(HPF_ERR_INVALID, "null list, or null labels with alpha < 1");

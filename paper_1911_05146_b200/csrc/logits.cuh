@@ -30,6 +30,7 @@ constexpr int kWarpRow = 1024;     // classes up to which a warp holds a row
 constexpr int kMaxParts = 8;       // CTAs a row is cut into (portable cluster size)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFloor = -1e30f;   // stands for -inf where it meets a weight of 0
+constexpr float kGone = -200.f;    // 2 to this is 0 in fp32
 
 __device__ __forceinline__ float ninf() { return __int_as_float(0xff800000); }
 // ---- element types ---------------------------------------------------------------------------------------------------
@@ -37,6 +38,7 @@ template <typename T> struct Io;
 template <> struct Io<float> {
     static constexpr int V = 4;
     static constexpr uint32_t kMinusInf = 0xff800000u;
+    static constexpr float kLowest = -3.4028235e38f, kBound = kFloor;      // the type's lowest value; what bounded() leaves at least
     static __device__ __forceinline__ void unpack(const uint4& r, float* f)
     {
         f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
@@ -84,6 +86,7 @@ struct Packed16 {
 template <> struct Io<__nv_bfloat16> : Packed16<__nv_bfloat16, __nv_bfloat162, 0xff7fff7fu, 0xf14af14au> {
     static constexpr int V = 8;
     static constexpr uint32_t kMinusInf = 0xff80ff80u;
+    static constexpr float kLowest = -3.3895314e38f, kBound = kFloor;
     static __device__ __forceinline__ void two(uint32_t w, float* f)
     {
         f[0] = __uint_as_float(w << 16);
@@ -108,6 +111,7 @@ template <> struct Io<__nv_bfloat16> : Packed16<__nv_bfloat16, __nv_bfloat162, 0
 template <> struct Io<__half> : Packed16<__half, __half2, 0xfbfffbffu, 0xfbfffbffu> {
     static constexpr int V = 8;
     static constexpr uint32_t kMinusInf = 0xfc00fc00u;
+    static constexpr float kLowest = -65504.f, kBound = -65504.f;
     static __device__ __forceinline__ void two(uint32_t w, float* f)
     {
         const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
@@ -208,8 +212,10 @@ struct Stretches {
 // bf16: 279 us instead of 190).
 constexpr int kNoHard = -1, kOwnExp = 0;
 
-// One thread's share of the row.  ENTROPY: -inf is replaced by the type's lowest value ahead of the weighted sum (0 (-inf) would be NaN);
-// v - m overflows only where m > 10^30, where every class but the largest weighs nothing: see write_stats.
+// One thread's share of the row.  ENTROPY: -inf is replaced by the type's lowest value (0 (-inf) would be NaN in the weighted sum) as long as
+// that is so far below the largest logit that it weighs 0 too; else (a strip of nothing but such masks, or a temperature of hundreds
+// in fp16) each class is looked at by itself.  v - m overflows only where m > 10^30, where every class but the largest weighs nothing: see
+// write_stats.
 template <typename T, int NT, bool ENTROPY, int POWER>
 __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, const Stretches* st)
 {
@@ -220,6 +226,8 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, c
     f2 s2 = 0, w2 = 0, h2 = 0;
     const f2 c2 = pair(c, c), one2 = pair(kLog2e, kLog2e);
     f2 base2 = 0;                                             // -m, twice
+    const auto near = [&](float m) { return ENTROPY && !((Io<T>::kLowest - m) * c < kGone); };
+    bool careful = near(0.f);
     int slot = 0, left = st ? st->iters : 0;
     float stretch = ninf();
     // one round: U pieces, of which the first `there` hold classes
@@ -245,6 +253,21 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, c
             }
             a.m = top;
             base2 = pair(-top, -top);
+            careful = near(top);
+        }
+        if (ENTROPY && careful) {
+            Sums b{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (u < there) {
+                    float f[V];
+                    Io<T>::unpack(raw[u], f);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) add_value<true, false>(b, f[j], c, base_of(a.m));
+                }
+            s2 = add2(s2, pair(b.s, 0.f));
+            w2 = add2(w2, pair(b.w, 0.f));
+            return;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -482,6 +505,8 @@ cudaError_t launch_warps(K* kernel, int64_t rows, cudaStream_t st, const A& args
 // ---- checks ----------------------------------------------------------------------------------------------------------
 int element(int32_t dtype) { return dtype == HPF_FP32 ? 4 : 2; }
 bool on(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+// 1 / T, and a masked class at the type's lowest value, stay far from the ends of fp32
+bool temperature_ok(float t) { return t >= 1e-30f && t <= 1e30f; }
 int check_rows(const void* logits, int64_t rows, int32_t classes, int64_t ld, int32_t dtype)
 {
     if (dtype != HPF_FP32 && dtype != HPF_BF16 && dtype != HPF_FP16) return api_fail(HPF_ERR_INVALID, "dtype must be HPF_FP32, HPF_BF16 or HPF_FP16");

@@ -415,7 +415,7 @@ struct LogprobsGrad {                // of one row: a class gets p (a + b (v - m
     float c, m, a, b, g_lp, g_h, h, inv_t;
     int label;
     bool dead;                       // nothing flows back: zeros, whatever the logits hold
-    bool far;                        // scales at which a class at -10^30 would weigh something, or its product with b overflow
+    bool far;                        // scales at which a class at `bound` (what stands for less) would weigh something, or its product with b overflow
     __device__ __forceinline__ LogprobsGrad(const LogprobsGradArgs& p, int64_t row)
     {
         label = p.labels ? p.labels[row] : -1;
@@ -427,7 +427,7 @@ struct LogprobsGrad {                // of one row: a class gets p (a + b (v - m
         c = p.inv_t * kLog2e;
         inv_t = p.inv_t;
     }
-    __device__ __forceinline__ void scale(const RowScale& s)
+    __device__ __forceinline__ void scale(const RowScale& s, float bound)
     {
         if (s.none) dead = true;
         m = s.m;
@@ -435,7 +435,7 @@ struct LogprobsGrad {                // of one row: a class gets p (a + b (v - m
         const float w = inv_t / s.s;
         a = -w * (g_lp + g_h * (h - logf(s.s)));
         b = -w * g_h * inv_t;
-        far = !(fabsf(m) < 1e29f) || !(fabsf(b) < 1e6f) || !(c > 1e-20f);
+        far = !(fabsf(m) < 1e29f) || !(fabsf(b) < 1e6f) || !((bound - m) * c < kGone);
     }
     __device__ __forceinline__ float slow(float v) const
     {
@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(NT) logprobs_bwd_kernel(const __grid_constant_
         if (p.parts > 1) a = cluster_sums<false>(a, g.c, part, p.parts, s_parts);
         s = scale_of(a);
     }
-    g.scale(s);
+    g.scale(s, Io<T>::kBound);
     __syncthreads();                                         // the label's logit has been read (the gradient may be written in its place)
     if (g.dead) write_row<T, NT, false, false>(sh, out, threadIdx.x, [](f2) { return (f2)0; });
     else if (g.far)
@@ -504,7 +504,7 @@ __global__ void __launch_bounds__(128) logprobs_bwd_warp_kernel(const __grid_con
     const float lse = p.lse[row];
     RowScale s{lse / p.inv_t, 1.f, false};
     if (!g.dead && !(fabsf(lse) < kLseExact)) s = scale_of(warp_run_over<T, false>(x, p.n, g.c, lane));
-    g.scale(s);
+    g.scale(s, Io<T>::kBound);
     for (int i0 = lane; i0 < p.n; i0 += 256) {               // eight loads under way (`out` may be x: they cannot pass the stores)
         float v[8];
 #pragma unroll
@@ -556,7 +556,7 @@ extern "C" int hpf_logprobs_fwd(const void* d_logits, const int32_t* d_labels, f
 {
     const int bad = check_rows(d_logits, rows, classes, ld, dtype);
     if (bad != HPF_OK) return bad;
-    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature)) return api_fail(HPF_ERR_INVALID, "the temperature must be positive");
+    if (!temperature_ok(temperature)) return api_fail(HPF_ERR_INVALID, "the temperature must lie in [1e-30, 1e30]");
     if (k < 0 || k > kMaxTop) return api_fail(HPF_ERR_UNSUPPORTED, "at most 64 classes are listed per row");
     if (rows == 0) return HPF_OK;
     if ((d_logprob && !d_labels) || (k && (!d_top_ids || !d_top_logprobs))) return api_fail(HPF_ERR_INVALID, "null labels, or k > 0 with a null list");
@@ -572,7 +572,7 @@ extern "C" int hpf_logprobs_bwd(const void* d_logits, const int32_t* d_labels, c
 {
     const int bad = check_rows(d_logits, rows, classes, ld, dtype);
     if (bad != HPF_OK) return bad;
-    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature)) return api_fail(HPF_ERR_INVALID, "the temperature must be positive");
+    if (!temperature_ok(temperature)) return api_fail(HPF_ERR_INVALID, "the temperature must lie in [1e-30, 1e30]");
     if (ld_d < classes) return api_fail(HPF_ERR_INVALID, "a row stride below the class count");
     if (rows == 0) return HPF_OK;
     if (!d_lse || !d_dlogits || !on(d_dlogits, element(dtype)) || (d_dlogprob && !d_labels) || (d_dentropy && !d_entropy))

@@ -168,6 +168,37 @@ def test_masked_and_broken_rows(rows, n, dtype):
     assert torch.all(d[4:] == 0)
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T", [1.0, 0.01, 300.0, 5000.0, 1e20])
+@pytest.mark.parametrize("rows, n", [(5, 200), (5, 3100), (600, 1300)])
+def test_masks_weigh_nothing_at_any_temperature(rows, n, T, dtype):
+    """-inf and the type's lowest value next to each other, alone and among ordinary logits; at 5000 the lowest fp16 value is no mask any more."""
+    x, _ = _logits(rows, n, dtype, n, 0, 41)
+    low = float(torch.finfo(TYPES[dtype]).min)
+    x[0, ::2] = float("-inf")
+    x[1] = float("-inf"); x[1, 3:50:4] = low
+    x[2, 1::2] = low; x[2, ::4] = float("-inf")
+    x[3, :] = low; x[3, n // 2:] = float("-inf")
+    v = x.double().cpu().numpy()
+    lab = np.full(rows, 3, np.int32)
+    labels = torch.from_numpy(lab).to(DEV)
+    got, o = _forward(x, labels, rows, n, n, 5, T)
+    want = ref.logprobs(v, lab, 5, T)
+    _close(got["entropy"], want["entropy"], STAT)
+    assert np.array_equal(got["ids"], want["ids"])
+    # -1e30 and below times 1 / T may leave fp32: both sides are compared as fp32 has them
+    as32 = lambda a: np.where(np.abs(a) > 3.4028235e38, np.sign(a) * np.inf, a)  # noqa: E731
+    with np.errstate(invalid="ignore"):
+        for key in ("logprob", "top"):
+            w = as32(want[key])
+            fine = np.isfinite(w)
+            _close(got[key], w, STAT + np.where(fine, np.abs(w), 0) * 2.0 ** -22)
+    ones, d = torch.ones(rows, device=DEV), torch.full_like(x, 9.0)
+    hpf.logprobs_bwd(x, labels, o["lse"], o["entropy"], ones, ones, d, rows, n, n, n, T)
+    dw = ref.logprobs_grad(v, lab, np.ones(rows), np.ones(rows), T)
+    _close(d.double().cpu().numpy(), dw, _grad_tol(dw, dtype, 20.0 / T))
+
+
 @pytest.mark.parametrize("shift", [0.0, 100.0, -1000.0, 30000.0])
 @pytest.mark.parametrize("rows, n", [(3, 300), (3, 2500), (200, 1500)])
 def test_large_logits_lose_nothing(rows, n, shift):

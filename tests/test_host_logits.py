@@ -17,7 +17,7 @@ def _fwd(**kw):
 @pytest.mark.parametrize("change, status", [
     (dict(logits=None), INVALID), (dict(labels=None), INVALID), (dict(ids=None), INVALID), (dict(lps=None), INVALID), (dict(rows=-1), INVALID),
     (dict(classes=0), INVALID), (dict(ld=9), INVALID), (dict(k=-1), UNSUPPORTED), (dict(k=65), UNSUPPORTED), (dict(t=0.0), INVALID),
-    (dict(t=-1.0), INVALID), (dict(t=float("nan")), INVALID), (dict(t=float("inf")), INVALID), (dict(t=1e-45), INVALID), (dict(dtype=3), INVALID),
+    (dict(t=-1.0), INVALID), (dict(t=float("nan")), INVALID), (dict(t=float("inf")), INVALID), (dict(t=1e-45), INVALID), (dict(t=1e31), INVALID), (dict(dtype=3), INVALID),
     (dict(logits=P + 2), INVALID), (dict(logits=P + 1, dtype=1), INVALID), (dict(rows=1 << 40), UNSUPPORTED)])
 def test_logprobs_fwd_refuses(change, status):
     assert _fwd(**change) == status
