@@ -1030,6 +1030,22 @@ struct Operand {
     bool mn;                         // the contiguous dimension is m / n
 };
 
+// A two-dimensional tensor map.  A host thread that has made no call of the runtime yet has no current context, which the driver's encoder wants:
+// cudaSetDevice makes the device's primary context current (and changes nothing where it is).
+cudaError_t encode_2d(CUtensorMap* tm, CUtensorMapDataType type, void* base, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+                      CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion)
+{
+    const cuuint32_t ones[2] = {1, 1};
+    for (int attempt = 0;; ++attempt) {
+        if (g_encode(tm, type, 2, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS)
+            return cudaSuccess;
+        if (attempt) return cudaErrorInvalidValue;
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e == cudaSuccess) e = cudaSetDevice(dev);
+        if (e != cudaSuccess) return e;
+    }
+}
 // box: rows of m / n of a k-contiguous stage
 template <int E>
 cudaError_t make_map(CUtensorMap* tm, const Operand& o, int32_t dtype, int box_rows)
@@ -1038,12 +1054,9 @@ cudaError_t make_map(CUtensorMap* tm, const Operand& o, int32_t dtype, int box_r
     const cuuint64_t dims[2] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows};
     const cuuint64_t strides[1] = {(cuuint64_t)(o.ld * E)};
     const cuuint32_t box[2] = {(cuuint32_t)inner, (cuuint32_t)(o.mn ? inner : box_rows)};
-    const cuuint32_t ones[2] = {1, 1};
     const CUtensorMapDataType type = dtype == HPF_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == HPF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    const CUresult r = g_encode(tm, type, 2, const_cast<void*>(o.p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                E == 4 && o.mn ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+    return encode_2d(tm, type, const_cast<void*>(o.p), dims, strides, box, E == 4 && o.mn ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B : CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
 // map of an output: copies of 32 x 32 blocks
@@ -1052,11 +1065,9 @@ cudaError_t make_out_map(CUtensorMap* tm, void* out, int64_t rows, int64_t cols,
 {
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)(ld * sizeof(T))};
-    const cuuint32_t box[2] = {32, 32}, ones[2] = {1, 1};
+    const cuuint32_t box[2] = {32, 32};
     const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == HPF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    const CUresult r = g_encode(tm, type, 2, out, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                sizeof(T) == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+    return encode_2d(tm, type, out, dims, strides, box, sizeof(T) == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
 }
 
 template <int E, typename T, int BN, bool PROMOTE>

@@ -304,3 +304,36 @@ def test_binding_refuses_what_the_kernels_would_misread():
         hpf.linear_fwd(c.x, c.w, None, None, c.y, None, *c.size, 0, c.scratch[:100])
     with pytest.raises(hpf.HpfError):
         hpf.linear_bwd(c.dy, None, c.x, c.w, c.dx, torch.zeros((24, 16), dtype=torch.float16, device=DEV), None, *c.size, 0, c.scratch)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows that start more than 2^32 elements into their buffers."""
+    rows, n_in, n_out, ld = 3, 40, 72, (1 << 31) + 8
+    t = torch.bfloat16
+    x, dx, y, dy = (torch.empty((rows - 1) * ld + n, dtype=t, device=DEV).as_strided((rows, n), (ld, 1)) for n in (n_in, n_in, n_out, n_out))
+    g = torch.Generator(device=DEV); g.manual_seed(1)
+    x.copy_(torch.randn(rows, n_in, generator=g, device=DEV)); dy.copy_(torch.randn(rows, n_out, generator=g, device=DEV))
+    w = torch.randn(n_out, n_in, generator=g, device=DEV).to(t)
+    dw, db = torch.empty_like(w), torch.empty(n_out, dtype=t, device=DEV)
+    size = (rows, n_in, n_out, ld, ld, hpf.ACT_NONE)
+    scratch = torch.zeros(hpf.linear_scratch_bytes(*size[:5], t), dtype=torch.uint8, device=DEV)
+    hpf.linear_fwd(x, w, None, None, y, None, *size, scratch)
+    hpf.linear_bwd(dy, None, x, w, dx, dw, db, *size, scratch)
+    torch.cuda.synchronize()
+    X, W, D = x.double(), w.double(), dy.double()
+    for got, want, size_ in ((y, X @ W.T, X.abs() @ W.abs().T), (dx, D @ W, D.abs() @ W.abs()), (dw, D.T @ X, D.abs().T @ X.abs()), (db, D.sum(0), D.abs().sum(0))):
+        _within(got, want, _half(t) * want.abs() + 2.0 ** -20 * size_, "offsets")
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_behind_the_last_are_left_alone(dtype):
+    """y, z and dx larger than the batch: what lies behind its last row stays as it was."""
+    rows, n_in, n_out, more = 130, 64, 96, 3
+    c = Case(rows, n_in, n_out, dtype, hpf.ACT_GELU)
+    y, z, dx = (torch.full((rows + more, n), 5.0, dtype=c.t, device=DEV) for n in (n_out, n_out, n_in))
+    hpf.linear_fwd(c.x, c.w, c.bias, c.residual, y, z, *c.size, c.act, c.scratch)
+    hpf.linear_bwd(c.dy, c.z, c.x, c.w, dx, None, None, *c.size, c.act, c.scratch)
+    c.forward(); c.backward()
+    torch.cuda.synchronize()
+    for big, small in ((y, c.y), (z, c.z_out), (dx, c.dx)):
+        assert torch.equal(big[:rows], small) and (big[rows:] == 5.0).all()
