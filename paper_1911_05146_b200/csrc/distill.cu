@@ -169,6 +169,7 @@ __device__ __forceinline__ void write_listed(const DistillArgs& p, const Teacher
 template <typename T, int NT, bool HARD, bool FWD, bool BWD>
 __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const __grid_constant__ DistillArgs p)
 {
+    enter();
     __shared__ Sums s_part[32];
     __shared__ Sums s_parts[kMaxParts];
     __shared__ Teacher s_teacher;
@@ -238,6 +239,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const __grid_con
 template <typename T, int J, bool HARD, bool FWD, bool BWD>
 __global__ void __launch_bounds__(128) distill_warp_kernel(const __grid_constant__ DistillArgs p)
 {
+    enter();
     __shared__ Teacher s_teacher[4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = (int64_t)blockIdx.x * 4 + warp;

@@ -33,6 +33,14 @@ constexpr float kFloor = -1e30f;   // stands for -inf where it meets a weight of
 constexpr float kGone = -200.f;    // 2 to this is 0 in fp32
 
 __device__ __forceinline__ float ninf() { return __int_as_float(0xff800000); }
+// The first step of every kernel: they are launched as programmatic dependents, set up while their predecessor in the stream drains, and wait here
+// for its results.
+__device__ __forceinline__ void enter()
+{
+    pdl_launch_dependents();
+    pdl_wait();
+}
+
 // ---- element types ---------------------------------------------------------------------------------------------------
 template <typename T> struct Io;
 template <> struct Io<float> {
@@ -483,12 +491,14 @@ cudaError_t launch_rows(K* kernel, int64_t rows, int parts, int threads, cudaStr
     cfg.gridDim = dim3((unsigned)(rows * parts));
     cfg.blockDim = dim3(threads);
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)parts;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)parts;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = parts > 1 ? 1 : 0;
+    cfg.numAttrs = parts > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 // Rows per SM from which CTAs of 128 threads take them: eight rows at different steps hide each other's waits better than four (4096 x 50021
@@ -498,8 +508,7 @@ constexpr int kManyRows = 4;
 template <typename K, typename A>
 cudaError_t launch_warps(K* kernel, int64_t rows, cudaStream_t st, const A& args)
 {
-    kernel<<<(unsigned)((rows + 3) / 4), 128, 0, st>>>(args);
-    return cudaGetLastError();
+    return launch_rows(kernel, (rows + 3) / 4, 1, 128, st, args);
 }
 
 // ---- checks ----------------------------------------------------------------------------------------------------------

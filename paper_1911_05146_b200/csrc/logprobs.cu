@@ -247,6 +247,7 @@ __device__ __forceinline__ void write_stats(const LogprobsArgs& p, int64_t row, 
 template <typename T, int NT, bool TOP>
 __global__ void __launch_bounds__(NT, 1024 / NT) logprobs_fwd_kernel(const __grid_constant__ LogprobsArgs p)
 {
+    enter();
     constexpr bool PARTS = NT == 512;                   // a row is cut into parts only where few rows leave the CTAs large
     __shared__ Sums s_part[32];
     __shared__ Sums s_parts[kMaxParts];
@@ -299,10 +300,14 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprobs_fwd_kernel(const __gri
             const float ln_s = logf(a.s);
             const int total = p.parts * p.k;
             for (int i = threadIdx.x; i < total; i += NT) {
-                // the parts' lists are in order: a class's place is the number of larger keys in each
                 const unsigned long long mine = s_all[i];
                 int rank = 0;
-                for (int q = 0; q < p.parts; ++q) {
+                if (total <= 256) {
+#pragma unroll 8
+                    for (int j = 0; j < total; ++j) rank += s_all[j] > mine;
+                }
+                // the parts' lists are in order: a class's place is the number of larger keys in each
+                for (int q = 0; total > 256 && q < p.parts; ++q) {
                     const unsigned long long* list = s_all + q * p.k;
                     int lo = 0;                              // keys before lo are larger
 #pragma unroll
@@ -325,6 +330,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprobs_fwd_kernel(const __gri
 template <typename T, int J>
 __global__ void __launch_bounds__(128) logprobs_fwd_warp_kernel(const __grid_constant__ LogprobsArgs p)
 {
+    enter();
     const int lane = threadIdx.x & 31;
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (row >= p.rows) return;
@@ -452,6 +458,7 @@ struct LogprobsGrad {                // of one row: a class gets p (a + b (v - m
 template <typename T, int NT>
 __global__ void __launch_bounds__(NT) logprobs_bwd_kernel(const __grid_constant__ LogprobsGradArgs p)
 {
+    enter();
     __shared__ Sums s_part[32];
     __shared__ Sums s_parts[kMaxParts];
     const int part = (int)(blockIdx.x % (unsigned)p.parts);
@@ -495,6 +502,7 @@ __device__ __forceinline__ Sums warp_run_over(const T* x, int n, float c, int la
 template <typename T>
 __global__ void __launch_bounds__(128) logprobs_bwd_warp_kernel(const __grid_constant__ LogprobsGradArgs p)
 {
+    enter();
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (row >= p.rows) return;
     const int lane = threadIdx.x & 31;
