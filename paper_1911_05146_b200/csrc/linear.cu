@@ -1139,16 +1139,18 @@ struct Plan {
     int bn, split;
 };
 // Tile width and split of k by a modelled time in clocks: waves of CTAs x (stages a CTA runs through x clocks of a stage + what a tile
-// costs besides).  A stage takes its MMAs (M = 128: 39 clocks at N = 32, 48 at 64, 64 at 128, 128 at 256) or its copies at 48 bytes a
-// clock, what L2 gave every SM at once, whichever is longer.
-Plan choose(int64_t lanes, int64_t cols, int k_blocks, int narrowest, int widest, int mmas, const Fit& fit)
+// costs besides).  A stage takes its MMAs (M = 128: 39 clocks at N = 32, 48 at 64, 64 at 128, 128 at 256), its copies at 48 bytes a clock,
+// what L2 gave every SM at once, or, with fp32 operands, what goes through shared memory at 128 bytes a clock (copied in, lo parts
+// formed, three products read: 768 bytes a row of a stage), whichever is longest.
+Plan choose(int64_t lanes, int64_t cols, int k_blocks, int narrowest, int widest, bool fp32, const Fit& fit)
 {
     Plan best{widest, 1};
     double least = 1e300;
     for (int bn = widest; bn >= narrowest; bn /= 2) {
         const int64_t tiles = ((lanes + kTileM - 1) / kTileM) * ((cols + bn - 1) / bn);
-        const double products = mmas * (bn == 256 ? 128.0 : bn == 128 ? 64.0 : bn == 64 ? 48.0 : 39.0), copies = (kTileM + bn) * kRow / 48.0;
-        const double stage = products > copies ? products : copies;
+        const double products = (fp32 ? 12 : 4) * (bn == 256 ? 128.0 : bn == 128 ? 64.0 : bn == 64 ? 48.0 : 39.0), copies = (kTileM + bn) * kRow / 48.0;
+        const double shared = fp32 ? (kTileM + bn) * 6.0 : 0.0;
+        const double stage = products > copies ? (products > shared ? products : shared) : copies > shared ? copies : shared;
         for (int i = 0, split = 1; split <= kMaxSplit; ++i, split *= 2) {
             if (split > 1 && (bn == 256 || k_blocks < 2 * split || tiles > 2 * fit.clusters[i])) break;      // (two versions of 256 columns do not fit the ring)
             const int64_t waves = (tiles + fit.clusters[i] - 1) / fit.clusters[i];
@@ -1197,7 +1199,7 @@ cudaError_t gemm(GemmArgs& g, Operand a, Operand b, int64_t rows, int64_t cols, 
         across = rows;
     }
     g.k_blocks = (int)((K * E + kRow - 1) / kRow);
-    const Plan plan = choose(lanes, across, g.k_blocks, g.swap ? 32 : 64, g.swap ? (across <= 32 ? 32 : 64) : promote ? 128 : 256, E == 4 ? 12 : 4, fit);
+    const Plan plan = choose(lanes, across, g.k_blocks, g.swap ? 32 : 64, g.swap ? (across <= 32 ? 32 : 64) : promote ? 128 : 256, E == 4, fit);
     g.split = plan.split;
     g.tiles_m = (int)((lanes + kTileM - 1) / kTileM);
     g.tiles_n = (int)((across + plan.bn - 1) / plan.bn);
