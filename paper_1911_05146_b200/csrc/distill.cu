@@ -29,13 +29,18 @@ struct Entry {                       // one entry of the list, with the student'
     float t, v;
     __device__ __forceinline__ bool holds() const { return id >= 0 && !(t == ninf()); }
 };
-template <typename T>
-__device__ __forceinline__ Entry read_entry(const DistillArgs& p, const T* x, int64_t row, int j)
+// In two steps, the second of which needs what the first has fetched.
+__device__ __forceinline__ void fetch_entry(const DistillArgs& p, int64_t row, int j, Entry* e)
 {
-    const int id = p.ids[row * p.k + j];
-    const float t = p.teacher[row * p.k + j];
-    const bool there = id >= 0 && id < p.n;
-    return Entry{there ? id : -1, there ? t : ninf(), there ? Io<T>::get(x[id]) : 0.f};
+    e->id = p.ids[row * p.k + j];
+    e->t = p.teacher[row * p.k + j];
+}
+template <typename T>
+__device__ __forceinline__ void finish_entry(const DistillArgs& p, const T* x, Entry* e)
+{
+    const bool there = e->id >= 0 && e->id < p.n;
+    e->v = there ? Io<T>::get(x[e->id]) : 0.f;
+    if (!there) *e = Entry{-1, ninf(), 0.f};
 }
 __device__ __forceinline__ void put_entry(Teacher& t, int j, const Entry& e)
 {
@@ -186,12 +191,18 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < ENTRIES; ++i) {
         entry[i] = Entry{-1, ninf(), 0.f};
-        if ((int)threadIdx.x + i * NT < p.k) entry[i] = read_entry<T>(p, x, row, threadIdx.x + i * NT);
+        if ((int)threadIdx.x + i * NT < p.k) fetch_entry(p, row, threadIdx.x + i * NT, &entry[i]);
     }
     const int label = HARD ? p.labels[row] : -1;
     const bool there = HARD && label >= 0 && label < p.n;
-    const float label_v = there ? Io<T>::get(x[label]) : 0.f;
+    float label_v = 0.f;
     const float d_loss = BWD ? p.d_loss[row] : 0.f;
+    const auto gather = [&]() {
+#pragma unroll
+        for (int i = 0; i < ENTRIES; ++i)
+            if ((int)threadIdx.x + i * NT < p.k) finish_entry<T>(p, x, &entry[i]);
+        if (there) label_v = Io<T>::get(x[label]);
+    };
     RowStats st;
     bool form = FWD;                         // the same for every part of a row
     if constexpr (!FWD) {
@@ -200,7 +211,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const __grid_con
         form = !enough;
     }
     Sums a{ninf(), 0.f, 0.f, 0.f};
-    if (form) a = run_over_power<T, NT, HARD>(sh, c, threadIdx.x, p.power);
+    if (form) a = run_over_power<T, NT, HARD>(sh, c, threadIdx.x, p.power, gather);
+    else gather();
 #pragma unroll
     for (int i = 0; i < ENTRIES; ++i) {
         if ((int)threadIdx.x + i * NT < p.k) put_entry(s_teacher, threadIdx.x + i * NT, entry[i]);
@@ -257,7 +269,9 @@ __global__ void __launch_bounds__(128) distill_warp_kernel(const __grid_constant
     }
     bool holds = false;
     for (int j = lane; j < p.k; j += 32) {
-        const Entry e = read_entry<T>(p, x, row, j);
+        Entry e;
+        fetch_entry(p, row, j, &e);
+        finish_entry<T>(p, x, &e);
         put_entry(s_teacher[warp], j, e);
         holds = holds || e.holds();
     }
@@ -295,14 +309,14 @@ template <typename T, int NT, bool HARD, bool FWD, bool BWD>
 cudaError_t distill_rows(DistillArgs& a, cudaStream_t st)
 {
     auto* kernel = distill_kernel<T, NT, HARD, FWD, BWD>;
-    return launch_rows(kernel, a.rows, a.parts, NT, st, a);
+    return launch_rows(kernel, a.rows, a.parts, NT, st, a, (size_t)a.rows * a.n * sizeof(T));
 }
 template <typename T, bool HARD, bool FWD, bool BWD>
 cudaError_t distill_one(DistillArgs& a, cudaStream_t st)
 {
-    if (a.n <= 32) return launch_warps(distill_warp_kernel<T, 1, HARD, FWD, BWD>, a.rows, st, a);
-    if (a.n <= 256) return launch_warps(distill_warp_kernel<T, 8, HARD, FWD, BWD>, a.rows, st, a);
-    if (a.n <= kWarpRow) return launch_warps(distill_warp_kernel<T, 32, HARD, FWD, BWD>, a.rows, st, a);
+    if (a.n <= 32) return launch_warps(distill_warp_kernel<T, 1, HARD, FWD, BWD>, a.rows, st, a, (size_t)a.rows * a.n * sizeof(T));
+    if (a.n <= 256) return launch_warps(distill_warp_kernel<T, 8, HARD, FWD, BWD>, a.rows, st, a, (size_t)a.rows * a.n * sizeof(T));
+    if (a.n <= kWarpRow) return launch_warps(distill_warp_kernel<T, 32, HARD, FWD, BWD>, a.rows, st, a, (size_t)a.rows * a.n * sizeof(T));
     a.parts = parts_of(a.rows, a.n, sizeof(T));
     // Loss and gradient at once read a row twice, so the rows in work should fit L2: half as many of long ones (4096 rows of 256 KB: 445 us
     // with CTAs of 256, 412 with 512; of 100 KB: 165 and 200, 184 with 128; of 128 KB: 108 and 106; of 40 KB: 92 and 81 with 128).

@@ -33,8 +33,7 @@ constexpr float kFloor = -1e30f;   // stands for -inf where it meets a weight of
 constexpr float kGone = -200.f;    // 2 to this is 0 in fp32
 
 __device__ __forceinline__ float ninf() { return __int_as_float(0xff800000); }
-// The first step of every kernel: they are launched as programmatic dependents, set up while their predecessor in the stream drains, and wait here
-// for its results.
+// The first step of every kernel: where it is launched as a programmatic dependent (see launch_rows), it waits here for its predecessor's results.
 __device__ __forceinline__ void enter()
 {
     pdl_launch_dependents();
@@ -224,8 +223,9 @@ constexpr int kNoHard = -1, kOwnExp = 0;
 // that is so far below the largest logit that it weighs 0 too; else (a strip of nothing but such masks, or a temperature of hundreds
 // in fp16) each class is looked at by itself.  v - m overflows only where m > 10^30, where every class but the largest weighs nothing: see
 // write_stats.
-template <typename T, int NT, bool ENTROPY, int POWER>
-__device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, const Stretches* st)
+// between(): what else has to come from memory, asked for while the first pieces are under way.
+template <typename T, int NT, bool ENTROPY, int POWER, typename F>
+__device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, const Stretches* st, F&& between)
 {
     constexpr int V = Io<T>::V, U = 4;
     constexpr bool HARD = POWER != kNoHard;
@@ -314,6 +314,7 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, c
     } else {
         load_rest(raw);
     }
+    between();
 #pragma unroll 2
     for (int r = 0; r < full; ++r) {
         at += U * NT;
@@ -345,15 +346,15 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, c
     }
     return a;
 }
-template <typename T, int NT, bool HARD>
-__device__ __forceinline__ Sums run_over_power(const Share<T>& sh, float c, int tid, int power)
+template <typename T, int NT, bool HARD, typename F>
+__device__ __forceinline__ Sums run_over_power(const Share<T>& sh, float c, int tid, int power, F&& between)
 {
-    if constexpr (!HARD) return run_over<T, NT, false, kNoHard>(sh, c, tid, nullptr);
-    if (power == 1) return run_over<T, NT, false, 1>(sh, c, tid, nullptr);
-    if (power == 2) return run_over<T, NT, false, 2>(sh, c, tid, nullptr);
-    if (power == 3) return run_over<T, NT, false, 3>(sh, c, tid, nullptr);
-    if (power == 4) return run_over<T, NT, false, 4>(sh, c, tid, nullptr);
-    return run_over<T, NT, false, kOwnExp>(sh, c, tid, nullptr);
+    if constexpr (!HARD) return run_over<T, NT, false, kNoHard>(sh, c, tid, nullptr, between);
+    if (power == 1) return run_over<T, NT, false, 1>(sh, c, tid, nullptr, between);
+    if (power == 2) return run_over<T, NT, false, 2>(sh, c, tid, nullptr, between);
+    if (power == 3) return run_over<T, NT, false, 3>(sh, c, tid, nullptr, between);
+    if (power == 4) return run_over<T, NT, false, 4>(sh, c, tid, nullptr, between);
+    return run_over<T, NT, false, kOwnExp>(sh, c, tid, nullptr, between);
 }
 
 template <bool ENTROPY, bool HARD>
@@ -484,21 +485,31 @@ int parts_of(int64_t rows, int n, size_t elem)
     while (parts < kMaxParts && rows * parts * 2 <= sm_count() && (size_t)n * elem / (2 * parts) >= 8192) parts *= 2;
     return parts;
 }
+// As a programmatic dependent a kernel is scheduled while its predecessor in the stream drains.  That saves 0.5 us of a small call and 2 of a large
+// one, but CTAs that fill up what a predecessor of one wave leaves free share the SMs unevenly (777 x 32003 fp16, loss and gradient: 23 -> 28 us):
+// it is done below 2 MB of logits and from three waves on.
 template <typename K, typename A>
-cudaError_t launch_rows(K* kernel, int64_t rows, int parts, int threads, cudaStream_t st, const A& args)
+cudaError_t launch_rows(K* kernel, int64_t rows, int parts, int threads, cudaStream_t st, const A& args, size_t bytes)
 {
+    const bool dependent = bytes < (2u << 20) || rows * parts * threads >= (int64_t)3 * 1024 * sm_count();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * parts));
     cfg.blockDim = dim3(threads);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)parts;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    int n = 0;
+    if (dependent) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (parts > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)parts;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = parts > 1 ? 2 : 1;
+    cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 // Rows per SM from which CTAs of 128 threads take them: eight rows at different steps hide each other's waits better than four (4096 x 50021
@@ -506,9 +517,9 @@ cudaError_t launch_rows(K* kernel, int64_t rows, int parts, int threads, cudaStr
 constexpr int kManyRows = 4;
 
 template <typename K, typename A>
-cudaError_t launch_warps(K* kernel, int64_t rows, cudaStream_t st, const A& args)
+cudaError_t launch_warps(K* kernel, int64_t rows, cudaStream_t st, const A& args, size_t bytes)
 {
-    return launch_rows(kernel, (rows + 3) / 4, 1, 128, st, args);
+    return launch_rows(kernel, (rows + 3) / 4, 1, 128, st, args, bytes);
 }
 
 // ---- checks ----------------------------------------------------------------------------------------------------------

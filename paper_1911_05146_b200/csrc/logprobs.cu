@@ -222,8 +222,14 @@ __device__ __forceinline__ void write_top(const LogprobsArgs& p, int64_t row, in
     p.top_ids[row * p.k + rank] = key ? key_class(key) : -1;
     p.top_logprobs[row * p.k + rank] = key ? (key_value(key) - m) * p.inv_t - ln_s : ninf();
 }
+// The label's logit, if it is wanted and there is a label (else `there` is false).
 template <typename T>
-__device__ __forceinline__ void write_stats(const LogprobsArgs& p, int64_t row, const Sums& a)
+__device__ __forceinline__ float label_logit(const LogprobsArgs& p, int64_t row, int label, bool* there)
+{
+    *there = label >= 0 && label < p.n;
+    return *there ? Io<T>::get(reinterpret_cast<const T*>(p.logits)[row * p.ld + label]) : 0.f;
+}
+__device__ __forceinline__ void write_stats(const LogprobsArgs& p, int64_t row, const Sums& a, float label_v, bool label_there)
 {
     // a row without a finite logit has no distribution: a.m = -inf, a.s = 0
     const bool none = a.m == ninf() && a.s == 0.f;
@@ -233,11 +239,9 @@ __device__ __forceinline__ void write_stats(const LogprobsArgs& p, int64_t row, 
     if (p.lse) p.lse[row] = none ? ninf() : fmaf(a.m, p.inv_t, ln_s);
     if (p.entropy) p.entropy[row] = none ? 0.f : fmaf(-p.inv_t, w / a.s, ln_s);
     if (p.logprob) {
-        const int label = p.labels[row];
         float lp = 0.f;
-        if (label >= 0 && label < p.n) {
-            const float v = Io<T>::get(reinterpret_cast<const T*>(p.logits)[row * p.ld + label]);
-            lp = none || v == ninf() ? ninf() : (v - a.m) * p.inv_t - ln_s;
+        if (label_there) {
+            lp = none || label_v == ninf() ? ninf() : (label_v - a.m) * p.inv_t - ln_s;
             if (a.s != a.s) lp = a.s;
         }
         p.logprob[row] = lp;
@@ -265,14 +269,18 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprobs_fwd_kernel(const __gri
         st.count = TopShared<NT>::kStretches / NT;
         st.iters = (rounds + st.count - 1) / st.count;
     }
-    Sums a = run_over<T, NT, true, kNoHard>(sh, c, threadIdx.x, TOP ? &st : nullptr);
+    // (the label's logit would be two waits at the row's end, while everybody else has left)
+    const int label = p.logprob && threadIdx.x == 0 ? p.labels[row] : -1;
+    bool label_there = false;
+    float label_v = 0.f;
+    Sums a = run_over<T, NT, true, kNoHard>(sh, c, threadIdx.x, TOP ? &st : nullptr, [&]() { label_v = label_logit<T>(p, row, label, &label_there); });
     const float my_max = a.m;
     a = block_sums<NT, true, false>(a, c, s_part);
     // the strips' maxima leave the row's ends out: they are always looked at again
     int count = 0;
     if constexpr (TOP) count = select_top<T, NT>(sh, my_max, p.k, st.iters, sm);
     if (!PARTS || p.parts == 1) {
-        if (threadIdx.x == 0) write_stats<T>(p, row, a);
+        if (threadIdx.x == 0) write_stats(p, row, a, label_v, label_there);
         if constexpr (TOP) {
             const float ln_s = logf(a.s);
             for (int i = threadIdx.x; i < count; i += NT)
@@ -295,7 +303,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprobs_fwd_kernel(const __gri
         if (part) return;
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         a = join_sums<true, false>(s_parts, p.parts, threadIdx.x & 31, c);
-        if (threadIdx.x == 0) write_stats<T>(p, row, a);
+        if (threadIdx.x == 0) write_stats(p, row, a, label_v, label_there);
         if constexpr (TOP) {
             const float ln_s = logf(a.s);
             const int total = p.parts * p.k;
@@ -338,18 +346,20 @@ __global__ void __launch_bounds__(128) logprobs_fwd_warp_kernel(const __grid_con
     const float c = p.inv_t * kLog2e;
     float v[J];
     Sums a{ninf(), 0.f, 0.f, 0.f};
+    const int label = p.logprob && lane == 0 ? p.labels[row] : -1;
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-        v[j] = lane + 32 * j < p.n ? Io<T>::get(x[lane + 32 * j]) : ninf();
-        a.m = fmaxf(a.m, v[j]);
-    }
+    for (int j = 0; j < J; ++j) v[j] = lane + 32 * j < p.n ? Io<T>::get(x[lane + 32 * j]) : ninf();
+    bool label_there;
+    const float label_v = label_logit<T>(p, row, label, &label_there);
+#pragma unroll
+    for (int j = 0; j < J; ++j) a.m = fmaxf(a.m, v[j]);
 #pragma unroll
     for (int d = 16; d; d >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xffffffffu, a.m, d));
     const float base = base_of(a.m);
 #pragma unroll
     for (int j = 0; j < J; ++j) add_value<true, false>(a, v[j], c, base);
     a = warp_sums<true, false>(a, c);
-    if (lane == 0) write_stats<T>(p, row, a);
+    if (lane == 0) write_stats(p, row, a, label_v, label_there);
     if (p.k == 0) return;
     const float ln_s = logf(a.s);
     if constexpr (J > 1) {
@@ -470,7 +480,7 @@ __global__ void __launch_bounds__(NT) logprobs_bwd_kernel(const __grid_constant_
     const float lse = p.lse[row];
     RowScale s{lse / p.inv_t, 1.f, false};
     if (!g.dead && !(fabsf(lse) < kLseExact)) {              // the same for every part of a row
-        Sums a = block_sums<NT, false, false>(run_over<T, NT, false, kNoHard>(sh, g.c, threadIdx.x, nullptr), g.c, s_part);
+        Sums a = block_sums<NT, false, false>(run_over<T, NT, false, kNoHard>(sh, g.c, threadIdx.x, nullptr, []() {}), g.c, s_part);
         if (p.parts > 1) a = cluster_sums<false>(a, g.c, part, p.parts, s_parts);
         s = scale_of(a);
     }
@@ -529,28 +539,28 @@ __global__ void __launch_bounds__(128) logprobs_bwd_warp_kernel(const __grid_con
 template <typename T>
 cudaError_t logprobs_fwd(LogprobsArgs& a, cudaStream_t st)
 {
-    if (a.n <= 32) return launch_warps(logprobs_fwd_warp_kernel<T, 1>, a.rows, st, a);
-    if (a.n <= 256) return launch_warps(logprobs_fwd_warp_kernel<T, 8>, a.rows, st, a);
-    if (a.n <= kWarpRow) return launch_warps(logprobs_fwd_warp_kernel<T, 32>, a.rows, st, a);
+    if (a.n <= 32) return launch_warps(logprobs_fwd_warp_kernel<T, 1>, a.rows, st, a, (size_t)a.rows * a.n * sizeof(T));
+    if (a.n <= 256) return launch_warps(logprobs_fwd_warp_kernel<T, 8>, a.rows, st, a, (size_t)a.rows * a.n * sizeof(T));
+    if (a.n <= kWarpRow) return launch_warps(logprobs_fwd_warp_kernel<T, 32>, a.rows, st, a, (size_t)a.rows * a.n * sizeof(T));
     a.parts = parts_of(a.rows, a.n, sizeof(T));
     if (a.parts > 1) {
-        if (a.k) return launch_rows(logprobs_fwd_kernel<T, 512, true>, a.rows, a.parts, 512, st, a);
-        return launch_rows(logprobs_fwd_kernel<T, 512, false>, a.rows, a.parts, 512, st, a);
+        if (a.k) return launch_rows(logprobs_fwd_kernel<T, 512, true>, a.rows, a.parts, 512, st, a, (size_t)a.rows * a.n * sizeof(T));
+        return launch_rows(logprobs_fwd_kernel<T, 512, false>, a.rows, a.parts, 512, st, a, (size_t)a.rows * a.n * sizeof(T));
     }
     // (longer rows would have stretches of more than one round, 1.06 of the time with 256 threads at 256 KB)
     if (a.rows >= kManyRows * sm_count() && (size_t)a.n * sizeof(T) <= TopShared<128>::kStretches * 64) {
-        if (a.k) return launch_rows(logprobs_fwd_kernel<T, 128, true>, a.rows, 1, 128, st, a);
-        return launch_rows(logprobs_fwd_kernel<T, 128, false>, a.rows, 1, 128, st, a);
+        if (a.k) return launch_rows(logprobs_fwd_kernel<T, 128, true>, a.rows, 1, 128, st, a, (size_t)a.rows * a.n * sizeof(T));
+        return launch_rows(logprobs_fwd_kernel<T, 128, false>, a.rows, 1, 128, st, a, (size_t)a.rows * a.n * sizeof(T));
     }
-    if (a.k) return launch_rows(logprobs_fwd_kernel<T, 256, true>, a.rows, 1, 256, st, a);
-    return launch_rows(logprobs_fwd_kernel<T, 256, false>, a.rows, 1, 256, st, a);
+    if (a.k) return launch_rows(logprobs_fwd_kernel<T, 256, true>, a.rows, 1, 256, st, a, (size_t)a.rows * a.n * sizeof(T));
+    return launch_rows(logprobs_fwd_kernel<T, 256, false>, a.rows, 1, 256, st, a, (size_t)a.rows * a.n * sizeof(T));
 }
 template <typename T>
 cudaError_t logprobs_bwd(LogprobsGradArgs& a, cudaStream_t st)
 {
-    if (a.n <= kWarpRow) return launch_warps(logprobs_bwd_warp_kernel<T>, a.rows, st, a);
+    if (a.n <= kWarpRow) return launch_warps(logprobs_bwd_warp_kernel<T>, a.rows, st, a, (size_t)a.rows * a.n * sizeof(T));
     a.parts = parts_of(a.rows, a.n, sizeof(T));
-    return launch_rows(logprobs_bwd_kernel<T, 256>, a.rows, a.parts, 256, st, a);
+    return launch_rows(logprobs_bwd_kernel<T, 256>, a.rows, a.parts, 256, st, a, (size_t)a.rows * a.n * sizeof(T));
 }
 
 }  // namespace
