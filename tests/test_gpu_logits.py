@@ -389,3 +389,63 @@ def test_offsets_beyond_32_bits():
     hpf.logprobs_bwd(x, labels, o["lse"], o["entropy"], one, one, x, rows, n, ld, ld, 1.0)
     dw = ref.logprobs_grad(v, lab, np.ones(rows), np.ones(rows), 1.0)
     _close(x.double().cpu().numpy(), dw, _grad_tol(dw, "bf16", 20.0))
+
+
+@pytest.mark.parametrize("alpha, T", [(1.0, 1.7), (0.4, 1.0), (0.4, 2.0), (0.4, 3.0), (0.4, 4.0), (0.4, 0.9)])
+@pytest.mark.parametrize("rows, n, ld, offset, dtype, k", [(1200, 33001, 33001, 0, "bf16", 20), (910, 120007, 120011, 3, "fp16", 64), (900, 62003, 62003, 1, "fp32", 200),
+                                                           (1000, 106496, 106496, 0, "bf16", 7), (893, 110001, 110003, 5, "bf16", 256)])
+def test_distill_of_many_long_rows(rows, n, ld, offset, dtype, k, alpha, T):
+    """Several waves of rows on either side of the lengths at which the CTAs change, from any alignment, with masked, broken and weightless rows among
+    them.  Sampled rows against 64 bits, all of them against the two separate calls; in place the same bits."""
+    t = TYPES[dtype]
+    g = torch.Generator(device=DEV); g.manual_seed(n)
+    buf = torch.full((offset + rows * ld,), 77.0, dtype=t, device=DEV)
+    x = buf[offset:].as_strided((rows, n), (ld, 1))
+    x.copy_(2.0 * torch.randn(rows, n, generator=g, device=DEV))
+    x[1] = float("-inf")
+    x[2, 5:] = float("-inf")
+    x[3, 7] = float("nan")
+    x[4] = torch.finfo(t).min
+    x[rows - 1] += 300.0
+    labels = torch.randint(n, (rows,), generator=g, device=DEV, dtype=torch.int32)
+    labels[::5] = -1
+    labels[2] = 3
+    ids = torch.randint(n, (rows, k), generator=g, device=DEV, dtype=torch.int32)
+    ids[2] = 1
+    ids[7] = -1
+    teacher = 3.0 * torch.randn(rows, k, generator=g, device=DEV)
+    w = torch.randn(rows, generator=g, device=DEV)
+    w[3] = 0.0
+    w[8] = 0.0
+    lab = labels if alpha < 1 else None
+    loss, loss2, stats = torch.full((rows,), 7.0, device=DEV), torch.full((rows,), 7.0, device=DEV), torch.empty((rows, 2), device=DEV)
+    ld_d = ld + 3
+    d = torch.full((rows, ld_d), 9.0, dtype=t, device=DEV)
+    d2 = torch.empty((rows, ld), dtype=t, device=DEV)
+    hpf.distill_fwd_bwd(x, lab, ids, teacher, w, loss, d, rows, n, ld, ld_d, k, T, alpha)
+    hpf.distill_fwd(x, lab, ids, teacher, loss2, stats, rows, n, ld, k, T, alpha)
+    hpf.distill_bwd(x, lab, ids, teacher, stats, w, d2, rows, n, ld, ld, k, T, alpha)
+    torch.cuda.synchronize()
+    assert (d[:, n:] == 9.0).all()
+    some = [0, 1, 2, 4, 5, 7, 8, 9, rows // 2, rows - 2, rows - 1]
+    pick = torch.tensor(some, device=DEV)
+    v = x[pick].double().cpu().numpy()
+    h = lambda a: a[pick].cpu().numpy()  # noqa: E731
+    loss_w, grad_w = ref.distill(v, h(labels), h(ids), h(teacher).astype(np.float64), h(w).astype(np.float64), T, alpha)
+    _close(loss[pick].double().cpu().numpy(), loss_w, 3e-5 * max(1.0, T * T) + 1e-5 * np.abs(np.where(np.isfinite(loss_w), loss_w, 0)))
+    gt = _grad_tol(grad_w, dtype, np.abs(h(w))[:, None] * max(1.0, T) * 3)
+    _close(d[pick][:, :n].double().cpu().numpy(), grad_w, gt)
+    # both ways are within their tolerance of the same value; rows of a few large probabilities apart, half a step of the type each
+    ok = torch.isfinite(loss2)
+    assert torch.equal(torch.isnan(loss), torch.isnan(loss2)) and torch.isnan(loss[3])
+    assert ((loss - loss2).abs()[ok] <= 6e-5 * max(1.0, T * T) + 2e-5 * loss2.abs()[ok]).all()
+    a, b = d[:, :n].float(), d2[:, :n].float()
+    step = float(torch.finfo(t).eps) + 4e-5
+    bound = step * torch.maximum(a.abs(), b.abs()) + 2e-6 * 3 * max(1.0, T) * w.abs()[:, None] + (2.0 ** -24 if dtype == "fp16" else 0.0)
+    assert ((a - b).abs() <= bound).all()
+    del a, b, bound, d2
+    loss3 = torch.empty(rows, device=DEV)
+    hpf.distill_fwd_bwd(x, lab, ids, teacher, w, loss3, x, rows, n, ld, ld, k, T, alpha)
+    torch.cuda.synchronize()
+    assert torch.equal(x, d[:, :n]) and torch.equal(loss3[ok], loss[ok])
+    assert (buf[:offset] == 77.0).all() and (ld == n or (buf[offset:].as_strided((rows - 1, ld - n), (ld, 1), offset + n) == 77.0).all())
