@@ -211,6 +211,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_kernel(const __grid_con
         form = !enough;
     }
     Sums a{ninf(), 0.f, 0.f, 0.f};
+    if (form && p.parts > 1) cluster_here();
     if (form) a = run_over_power<T, NT, HARD>(sh, c, threadIdx.x, p.power, gather);
     else gather();
 #pragma unroll

@@ -1130,7 +1130,7 @@ cudaError_t how_many_fit(Fit* fit)
             cfg.attrs = attr;
             cfg.numAttrs = 1;
             e = cudaOccupancyMaxActiveClusters(&f->clusters[i], kernel, &cfg);
-            if (e == cudaSuccess && f->clusters[i] < 1) f->clusters[i] = 1;
+            if (i == 0 && f->clusters[0] < 1) f->clusters[0] = 1;           // (a size of which none fits is not chosen)
         }
         return e;
     });

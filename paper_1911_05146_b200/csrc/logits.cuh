@@ -388,12 +388,17 @@ __device__ __forceinline__ Sums block_sums(Sums a, float c, Sums* s_part)
     __syncthreads();
     return join_sums<ENTROPY, HARD>(s_part, NT / 32, threadIdx.x & 31, c);
 }
+// Another CTA's shared memory may be written once that CTA runs: every thread says so early (cluster_here) and waits for the others before the
+// first write (cluster_all_here), by when they long have.
+__device__ __forceinline__ void cluster_here() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_all_here() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // The same value for every CTA of a row: each puts its sums into the shared memory of all (into, not out of: nobody has to stay for others
-// to read).  s_parts: one place per part.
+// to read).  s_parts: one place per part.  After cluster_here().
 template <bool HARD>
 __device__ __forceinline__ Sums cluster_sums(Sums a, float c, int part, int parts, Sums* s_parts)
 {
     cg::cluster_group cl = cg::this_cluster();
+    cluster_all_here();
     if ((int)threadIdx.x < parts) *cl.map_shared_rank(&s_parts[part], threadIdx.x) = a;
     cl.sync();
     return join_sums<false, HARD>(s_parts, parts, threadIdx.x & 31, c);

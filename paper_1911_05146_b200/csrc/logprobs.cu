@@ -257,6 +257,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprobs_fwd_kernel(const __gri
     __shared__ Sums s_parts[kMaxParts];
     __shared__ __align__(16) unsigned char s_top[TOP ? sizeof(TopShared<NT>) : 16];
     __shared__ unsigned long long s_all[TOP && PARTS ? kMaxParts * kMaxTop : 1];
+    if (PARTS && p.parts > 1) cluster_here();
     const int part = PARTS ? (int)(blockIdx.x % (unsigned)p.parts) : 0;
     const int64_t row = PARTS ? blockIdx.x / (unsigned)p.parts : blockIdx.x;
     const float c = p.inv_t * kLog2e;
@@ -292,6 +293,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprobs_fwd_kernel(const __gri
     if constexpr (PARTS) {
         // sums and lists go to the row's first CTA
         cg::cluster_group cl = cg::this_cluster();
+        cluster_all_here();
         if (threadIdx.x == 0) *cl.map_shared_rank(&s_parts[part], 0) = a;
         if constexpr (TOP) {
             unsigned long long* there = cl.map_shared_rank(s_all + part * p.k, 0);
@@ -480,6 +482,7 @@ __global__ void __launch_bounds__(NT) logprobs_bwd_kernel(const __grid_constant_
     const float lse = p.lse[row];
     RowScale s{lse / p.inv_t, 1.f, false};
     if (!g.dead && !(fabsf(lse) < kLseExact)) {              // the same for every part of a row
+        if (p.parts > 1) cluster_here();
         Sums a = block_sums<NT, false, false>(run_over<T, NT, false, kNoHard>(sh, g.c, threadIdx.x, nullptr, []() {}), g.c, s_part);
         if (p.parts > 1) a = cluster_sums<false>(a, g.c, part, p.parts, s_parts);
         s = scale_of(a);
