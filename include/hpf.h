@@ -413,7 +413,7 @@ int hpf_distill_fwd(const void *d_logits, const int32_t *d_labels, const int32_t
 int hpf_distill_bwd(const void *d_logits, const int32_t *d_labels, const int32_t *d_teacher_ids, const float *d_teacher_logits,
                     const float *d_stats, const float *d_dloss, void *d_dlogits, int64_t rows, int32_t classes, int64_t ld,
                     int64_t ld_d, int32_t k, float temperature, float alpha, int32_t dtype, void *stream);
-/* Both in one kernel, which reads the logits from memory once. */
+/* Both in one kernel, which reads the logits from memory once.  d_dlogits may be d_logits (with ld_d = ld). */
 int hpf_distill_fwd_bwd(const void *d_logits, const int32_t *d_labels, const int32_t *d_teacher_ids, const float *d_teacher_logits,
                         const float *d_dloss, float *d_loss, void *d_dlogits, int64_t rows, int32_t classes, int64_t ld,
                         int64_t ld_d, int32_t k, float temperature, float alpha, int32_t dtype, void *stream);

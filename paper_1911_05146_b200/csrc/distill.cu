@@ -341,7 +341,7 @@ int check_distill(const void* logits, const int32_t* labels, const int32_t* ids,
     if (!(alpha >= 0.f && alpha <= 1.f)) return api_fail(HPF_ERR_INVALID, "alpha must lie in [0, 1]");
     if (k < 0 || k > kMaxTeacher) return api_fail(HPF_ERR_UNSUPPORTED, "a teacher's list has at most 256 entries per row");
     if (rows && ((k && (!ids || !teacher)) || (alpha < 1.f && !labels))) return api_fail(HPF_ERR_INVALID, "null list, or null labels with alpha < 1");
-    return HPF_OK;
+    return check_words({labels, ids, teacher});
 }
 template <bool FWD, bool BWD>
 int distill_call(DistillArgs& a, int32_t dtype, void* stream)
@@ -366,6 +366,8 @@ extern "C" int hpf_distill_fwd(const void* d_logits, const int32_t* d_labels, co
     if (bad != HPF_OK) return bad;
     if (rows == 0) return HPF_OK;
     if (!d_loss) return api_fail(HPF_ERR_INVALID, "null argument");
+    const int words = check_words({d_loss, d_stats});
+    if (words != HPF_OK) return words;
     DistillArgs a{d_logits, d_labels, d_teacher_ids, d_teacher_logits, d_loss, d_stats, nullptr, nullptr, rows, ld, 0, classes, k, 1, temperature, 1.f / temperature, alpha, power_of(temperature)};
     return distill_call<true, false>(a, dtype, stream);
 }
@@ -378,7 +380,11 @@ extern "C" int hpf_distill_bwd(const void* d_logits, const int32_t* d_labels, co
     if (bad != HPF_OK) return bad;
     if (ld_d < classes) return api_fail(HPF_ERR_INVALID, "a row stride below the class count");
     if (rows == 0) return HPF_OK;
-    if (!d_stats || !d_dloss || !d_dlogits || !on(d_dlogits, element(dtype))) return api_fail(HPF_ERR_INVALID, "null argument");
+    if (!d_stats || !d_dloss) return api_fail(HPF_ERR_INVALID, "null argument");
+    const int words = check_words({d_stats, d_dloss});
+    if (words != HPF_OK) return words;
+    const int out = check_gradient(d_logits, d_dlogits, rows, ld, ld_d, dtype);
+    if (out != HPF_OK) return out;
     DistillArgs a{d_logits, d_labels, d_teacher_ids, d_teacher_logits, nullptr, const_cast<float*>(d_stats), d_dloss, d_dlogits, rows, ld, ld_d, classes, k, 1, temperature, 1.f / temperature, alpha, power_of(temperature)};
     return distill_call<false, true>(a, dtype, stream);
 }
@@ -391,7 +397,11 @@ extern "C" int hpf_distill_fwd_bwd(const void* d_logits, const int32_t* d_labels
     if (bad != HPF_OK) return bad;
     if (ld_d < classes) return api_fail(HPF_ERR_INVALID, "a row stride below the class count");
     if (rows == 0) return HPF_OK;
-    if (!d_loss || !d_dloss || !d_dlogits || !on(d_dlogits, element(dtype))) return api_fail(HPF_ERR_INVALID, "null argument");
+    if (!d_loss || !d_dloss) return api_fail(HPF_ERR_INVALID, "null argument");
+    const int words = check_words({d_loss, d_dloss});
+    if (words != HPF_OK) return words;
+    const int out = check_gradient(d_logits, d_dlogits, rows, ld, ld_d, dtype);
+    if (out != HPF_OK) return out;
     DistillArgs a{d_logits, d_labels, d_teacher_ids, d_teacher_logits, d_loss, nullptr, d_dloss, d_dlogits, rows, ld, ld_d, classes, k, 1, temperature, 1.f / temperature, alpha, power_of(temperature)};
     return distill_call<true, true>(a, dtype, stream);
 }

@@ -26,6 +26,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <initializer_list>
 #include <math.h>
 
 namespace cg = cooperative_groups;
@@ -1276,6 +1277,12 @@ int check(int64_t rows, int32_t n_in, int32_t n_out, int64_t ld_x, int64_t ld_y,
     return HPF_OK;
 }
 bool value_aligned(const void* p, int e) { return (reinterpret_cast<uintptr_t>(p) & (e - 1)) == 0; }
+bool any_of(const void* p, std::initializer_list<const void*> others)
+{
+    for (const void* o : others)
+        if (p && p == o) return true;
+    return false;
+}
 bool row_ok(const void* p, int64_t ld, int e) { return aligned16(p) && (ld * e) % 16 == 0; }
 
 }  // namespace
@@ -1307,6 +1314,7 @@ extern "C" int hpf_linear_fwd(const void* d_x, const void* d_w, const void* d_bi
     const bool x_ok = row_ok(d_x, ld_x, e), w_ok = row_ok(d_w, n_in, e);
     const Scratch s = scratch_of(rows, n_in, n_out, e, x_ok, w_ok, true, act, false);
     if (!aligned16(d_scratch) || scratch_bytes < s.total) return api_fail(HPF_ERR_WORKSPACE, "scratch too small or misaligned (hpf_linear_scratch_bytes)");
+    if (any_of(d_y, {d_x, d_w, d_bias}) || any_of(d_z, {d_x, d_w, d_bias, d_residual, d_y})) return api_fail(HPF_ERR_INVALID, "an output in an input's place");
     cudaError_t ce = conv_tc_init();
     if (ce != cudaSuccess) return api_cuda_fail(ce, "hpf_linear_fwd: set-up");
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -1345,6 +1353,8 @@ extern "C" int hpf_linear_bwd(const void* d_dy, const void* d_z, const void* d_x
     const bool products = d_dx || d_dw;
     const Scratch s = scratch_of(rows, n_in, n_out, e, x_ok, w_ok, dy_ok || !products, products ? act : HPF_ACT_NONE, true);
     if (!aligned16(d_scratch) || scratch_bytes < s.total) return api_fail(HPF_ERR_WORKSPACE, "scratch too small or misaligned (hpf_linear_scratch_bytes)");
+    if (any_of(d_dx, {d_dy, d_z, d_x, d_w, d_dw, d_dbias}) || any_of(d_dw, {d_dy, d_z, d_x, d_w, d_dbias}) || any_of(d_dbias, {d_dy, d_z, d_x, d_w}))
+        return api_fail(HPF_ERR_INVALID, "an output in an input's place");
     cudaError_t ce = conv_tc_init();
     if (ce != cudaSuccess) return api_cuda_fail(ce, "hpf_linear_bwd: set-up");
     char* base = static_cast<char*>(d_scratch);

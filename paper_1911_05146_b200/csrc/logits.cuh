@@ -19,6 +19,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <initializer_list>
 #include <math.h>
 
 namespace cg = cooperative_groups;
@@ -538,6 +539,20 @@ int check_rows(const void* logits, int64_t rows, int32_t classes, int64_t ld, in
     if (rows < 0 || classes < 1 || ld < classes) return api_fail(HPF_ERR_INVALID, "rows < 0, classes < 1 or a row stride below the class count");
     if (rows > 0x7fffffff / kMaxParts || classes > (1 << 30)) return api_fail(HPF_ERR_UNSUPPORTED, "more than 2^28 rows or 2^30 classes");
     if (rows && (!logits || !on(logits, element(dtype)))) return api_fail(HPF_ERR_INVALID, "logits: null or not aligned to their type");
+    return HPF_OK;
+}
+// Labels, lists and statistics are int32 and fp32 (null where a call has none).
+int check_words(std::initializer_list<const void*> all)
+{
+    for (const void* p : all)
+        if (!on(p, 4)) return api_fail(HPF_ERR_INVALID, "labels, lists or statistics not aligned to their type");
+    return HPF_OK;
+}
+// A gradient may take the logits' own place, row by row: then its rows are theirs.
+int check_gradient(const void* logits, const void* out, int64_t rows, int64_t ld, int64_t ld_d, int32_t dtype)
+{
+    if (!out || !on(out, element(dtype))) return api_fail(HPF_ERR_INVALID, "gradient: null or not aligned to its type");
+    if (out == logits && rows > 1 && ld_d != ld) return api_fail(HPF_ERR_INVALID, "a gradient in the logits' place needs their row stride");
     return HPF_OK;
 }
 

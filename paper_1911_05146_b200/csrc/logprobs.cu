@@ -581,6 +581,8 @@ extern "C" int hpf_logprobs_fwd(const void* d_logits, const int32_t* d_labels, f
     if (k < 0 || k > kMaxTop) return api_fail(HPF_ERR_UNSUPPORTED, "at most 64 classes are listed per row");
     if (rows == 0) return HPF_OK;
     if ((d_logprob && !d_labels) || (k && (!d_top_ids || !d_top_logprobs))) return api_fail(HPF_ERR_INVALID, "null labels, or k > 0 with a null list");
+    const int words = check_words({d_labels, d_logprob, d_entropy, d_lse, d_top_ids, d_top_logprobs});
+    if (words != HPF_OK) return words;
     LogprobsArgs a{d_logits, d_labels, d_logprob, d_entropy, d_lse, d_top_ids, d_top_logprobs, rows, ld, classes, k, 1, 1.f / temperature};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const cudaError_t e = dtype == HPF_FP32 ? logprobs_fwd<float>(a, st) : dtype == HPF_BF16 ? logprobs_fwd<__nv_bfloat16>(a, st) : logprobs_fwd<__half>(a, st);
@@ -596,8 +598,11 @@ extern "C" int hpf_logprobs_bwd(const void* d_logits, const int32_t* d_labels, c
     if (!temperature_ok(temperature)) return api_fail(HPF_ERR_INVALID, "the temperature must lie in [1e-30, 1e30]");
     if (ld_d < classes) return api_fail(HPF_ERR_INVALID, "a row stride below the class count");
     if (rows == 0) return HPF_OK;
-    if (!d_lse || !d_dlogits || !on(d_dlogits, element(dtype)) || (d_dlogprob && !d_labels) || (d_dentropy && !d_entropy))
-        return api_fail(HPF_ERR_INVALID, "null argument");
+    if (!d_lse || (d_dlogprob && !d_labels) || (d_dentropy && !d_entropy)) return api_fail(HPF_ERR_INVALID, "null argument");
+    const int words = check_words({d_labels, d_lse, d_entropy, d_dlogprob, d_dentropy});
+    if (words != HPF_OK) return words;
+    const int out = check_gradient(d_logits, d_dlogits, rows, ld, ld_d, dtype);
+    if (out != HPF_OK) return out;
     LogprobsGradArgs a{d_logits, d_labels, d_lse, d_entropy, d_dlogprob, d_dentropy, d_dlogits, rows, ld, ld_d, classes, 1, 1.f / temperature};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const cudaError_t e = dtype == HPF_FP32 ? logprobs_bwd<float>(a, st) : dtype == HPF_BF16 ? logprobs_bwd<__nv_bfloat16>(a, st) : logprobs_bwd<__half>(a, st);

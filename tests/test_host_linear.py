@@ -67,3 +67,17 @@ def test_scratch_holds_dz_and_what_a_copy_cannot_address(dtype, e):
     with pytest.raises(hpf.HpfError):
         hpf.linear_scratch_bytes(rows, 33, 51, 33, 51, torch.float64)
     assert hpf.lib().hpf_linear_scratch_bytes(1, 1, 1, 1, 1, 0, 0, 1, C.POINTER(C.c_size_t)()) == INVALID
+
+
+@pytest.mark.parametrize("change", [dict(y="x"), dict(y="w"), dict(y="bias"), dict(z="x"), dict(z="w"), dict(z="bias"), dict(z="residual"), dict(z="y")])
+def test_forward_refuses_an_output_in_an_inputs_place(change):
+    at = {name: P * (i + 1) for i, name in enumerate(["x", "w", "bias", "residual", "y", "z", "scratch"])}
+    at.update({name: at[other] for name, other in change.items()})
+    assert _fwd(**at) == INVALID
+
+
+@pytest.mark.parametrize("change", [{o: i} for o in ("dx", "dw", "db") for i in ("dy", "z", "x", "w")] + [dict(dx="dw"), dict(dx="db"), dict(dw="db")])
+def test_backward_refuses_an_output_in_an_inputs_place(change):
+    at = {name: P * (i + 1) for i, name in enumerate(["dy", "z", "x", "w", "dx", "dw", "db", "scratch"])}
+    at.update({name: at[other] for name, other in change.items()})
+    assert _bwd(**at) == INVALID

@@ -57,3 +57,20 @@ def test_distill_refuses(change, status):
     if "loss" not in change:
         assert L.hpf_distill_bwd(a["logits"], a["labels"], a["ids"], a["teacher"], P, a["w"], a["out"], 4, 10, 10, a["ld_d"], a["k"], a["t"], a["alpha"],
                                  a["dtype"], None) == status
+
+
+@pytest.mark.parametrize("name", ["labels", "logprob", "entropy", "lse", "ids", "lps"])
+def test_logprobs_fwd_refuses_words_off_their_boundary(name):
+    assert _fwd(**{name: P + 2}) == INVALID
+
+
+def test_gradients_refuse_words_off_their_boundary_and_another_stride_in_place():
+    L, other = hpf.lib(), 2 * P
+    for i in range(1, 6):
+        assert L.hpf_logprobs_bwd(*[P + 2 if j == i else P for j in range(6)], other, 4, 10, 10, 10, 1.0, 0, None) == INVALID
+        assert L.hpf_distill_bwd(*[P + 2 if j == i else P for j in range(6)], other, 4, 10, 10, 10, 4, 1.0, 0.5, 0, None) == INVALID
+        assert L.hpf_distill_fwd_bwd(*[P + 2 if j == i else P for j in range(6)], other, 4, 10, 10, 10, 4, 1.0, 0.5, 0, None) == INVALID
+        assert L.hpf_distill_fwd(*[P + 2 if j == i else P for j in range(6)], 4, 10, 10, 4, 1.0, 0.5, 0, None) == INVALID
+    assert L.hpf_logprobs_bwd(*[P] * 7, 4, 10, 10, 11, 1.0, 0, None) == INVALID
+    assert L.hpf_distill_bwd(*[P] * 7, 4, 10, 10, 11, 4, 1.0, 0.5, 0, None) == INVALID
+    assert L.hpf_distill_fwd_bwd(*[P] * 7, 4, 10, 12, 10, 4, 1.0, 0.5, 0, None) == INVALID
