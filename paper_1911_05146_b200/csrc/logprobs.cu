@@ -116,7 +116,8 @@ __device__ __forceinline__ float kth_of_four(const float (&value)[4], int k)
         if (count >= k) bound |= bit;
     }
     const uint32_t o = bound << 16;
-    return bound ? __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)) : ninf();
+    // (fewer than k values above -inf: cut to 16 bits, the key of -inf would be read back as a NaN, which nothing reaches)
+    return bound > order16(ninf()) ? __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)) : ninf();
 }
 
 // Of 128 groups of threads (t, t + 128, ...).

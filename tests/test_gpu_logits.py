@@ -125,6 +125,32 @@ def test_lists_of_rows_with_ties_and_of_sorted_rows(rows, n, k, dtype, kind):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("k", [1, 16, 17, 20, 63, 64])
+@pytest.mark.parametrize("rows, n", [(9, 20), (9, 51), (700, 51), (9, 250), (9, 1000), (9, 1500), (300, 2000), (700, 2000), (9, 60001), (600, 5001), (150, 70001)])
+def test_lists_with_fewer_classes_than_places(rows, n, k, dtype):
+    """Rows of few classes, and rows whose mask leaves fewer classes than the list has places, or just as many, spread out or side by side."""
+    x, _ = _logits(rows, n, dtype, n, 0, n + k)
+    v = x.double().cpu().numpy().copy()
+    rng = np.random.Generator(np.random.PCG64(k))
+    some = min(rows, 9)
+    for r, left in enumerate([n, 0, 1, k - 1, k, k + 1, k - 1, k, 2 * k][:some]):
+        left = min(left, n)
+        there = rng.choice(n, left, replace=False) if r < 6 else n // 2 - left // 2 + np.arange(left)
+        masked = np.ones(n, bool)
+        masked[there] = False
+        v[r, masked] = -np.inf
+    x.copy_(torch.from_numpy(v))
+    labels, lab = _labels(rows, n, 1)
+    got, _ = _forward(x, labels, rows, n, n, k, 1.0)
+    order = np.argsort(-v, axis=1, kind="stable")[:, :k]
+    want = np.full((rows, k), -1)
+    want[:, : order.shape[1]] = np.where(np.isfinite(np.take_along_axis(v, order, 1)), order, -1)
+    assert np.array_equal(got["ids"], want)
+    assert np.array_equal(np.isfinite(got["top"]), want >= 0) and not np.isnan(got["top"]).any()
+    _close(got["top"][:some], ref.logprobs(v[:some], lab[:some], k, 1.0)["top"], STAT)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("rows, n", [(6, 40), (6, 900), (6, 3001), (200, 1100)])
 def test_masked_and_broken_rows(rows, n, dtype):
     """Rows that a mask leaves empty or almost empty, the type's lowest value as a mask, +inf and NaN."""
