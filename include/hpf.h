@@ -382,7 +382,8 @@ int hpf_linear_fwd(const void *d_x, const void *d_w, const void *d_bias, const v
 int hpf_linear_bwd(const void *d_dy, const void *d_z, const void *d_x, const void *d_w, void *d_dx, void *d_dw, void *d_dbias, int64_t rows,
                    int32_t n_in, int32_t n_out, int64_t ld_x, int64_t ld_y, int32_t dtype, int32_t act, int32_t grad_type,
                    void *d_scratch, size_t scratch_bytes, void *stream);
-/* 1 if a bounded wait of a linear call on this scratch gave up since its head was zeroed (waits for those calls). */
+/* 1 if a bounded wait of a linear call on this scratch gave up since its head was zeroed (waits for the scratch's device, whatever the streams of
+ * those calls; not to be called while a stream is being captured). */
 int hpf_linear_status(const void *d_scratch, int32_t *h_gave_up);
 
 /* With s = logits / temperature:  d_lse = ln sum exp s;  d_logprob = s[label] - lse (0 without a label; -inf for a masked

@@ -434,7 +434,7 @@ def linear_bwd(dy, z, x, w, dx, dw, dbias, rows, n_in, n_out, ld_x, ld_y, act, s
 
 
 def linear_status(scratch):
-    """True if a bounded wait of a linear call on this scratch gave up (the scratch head must then be zeroed again)."""
+    """True if a bounded wait of a linear call on this scratch gave up (the scratch head must then be zeroed again); waits for its device."""
     v = _i32(); _check(lib().hpf_linear_status(_ptr(scratch), C.byref(v))); return bool(v.value)
 
 

@@ -87,6 +87,9 @@ __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;"
 // and hands the status back, so that every entry point, whichever file it lives in, reports through one place.
 int api_fail(int status, const char* what);
 int api_cuda_fail(cudaError_t e, const char* where);
+// Copies a few bytes of a scratch to the host once every stream of its device is idle: a copy on the legacy stream would not wait for streams
+// made non-blocking (all of torch's but the default one).
+cudaError_t read_when_idle(void* to, const void* d_from, size_t bytes);
 
 // Device-side status word shared by all kernels that have bounded waits.
 // 0 = fine; anything else = where a wait gave up (see conv_tc.cu).

@@ -33,6 +33,20 @@ int hpf::api_cuda_fail(cudaError_t e, const char* where)
     g_last_error = buf;
     return HPF_ERR_CUDA;
 }
+cudaError_t hpf::read_when_idle(void* to, const void* d_from, size_t bytes)
+{
+    int current = 0;
+    cudaPointerAttributes at = {};
+    cudaError_t e = cudaGetDevice(&current);
+    if (e == cudaSuccess) e = cudaPointerGetAttributes(&at, d_from);
+    if (e != cudaSuccess) return e;
+    const bool other = (at.type == cudaMemoryTypeDevice || at.type == cudaMemoryTypeManaged) && at.device != current;
+    if (other) e = cudaSetDevice(at.device);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpy(to, d_from, bytes, cudaMemcpyDeviceToHost);
+    if (other) (void)cudaSetDevice(current);
+    return e;
+}
 
 namespace {
 

@@ -1391,7 +1391,7 @@ extern "C" int hpf_linear_status(const void* d_scratch, int32_t* h_gave_up)
 {
     if (!d_scratch || !h_gave_up) return api_fail(HPF_ERR_INVALID, "null argument");
     DeviceStatus s = {};
-    const cudaError_t e = cudaMemcpy(&s, d_scratch, sizeof(s), cudaMemcpyDeviceToHost);
+    const cudaError_t e = read_when_idle(&s, d_scratch, sizeof(s));
     if (e != cudaSuccess) return api_cuda_fail(e, "hpf_linear_status");
     *h_gave_up = s.code != 0;
     return HPF_OK;
