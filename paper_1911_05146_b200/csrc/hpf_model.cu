@@ -1947,7 +1947,7 @@ int hpf_bnrelu_status(const void* d_scratch, int32_t* h_gave_up)
 {
     if (!d_scratch || !h_gave_up) return fail(HPF_ERR_INVALID, "null argument");
     unsigned int words[3] = {0, 0, 0};
-    CU(cudaMemcpy(words, d_scratch, sizeof words, cudaMemcpyDeviceToHost));
+    CU(read_when_idle(words, d_scratch, sizeof words));
     *h_gave_up = words[2] != 0u;
     return HPF_OK;
 }
