@@ -311,40 +311,61 @@ __device__ __forceinline__ void tma_store_wait()
 {
     asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
 }
+// A copy out writes whole 16-byte units, also past the last column of its tensor: what of a row's last unit is in `out` is left to the lanes.
+template <typename T>
+__device__ __forceinline__ int whole_columns(int cols) { return cols & -Pack<T>::V; }
+// The columns behind the whole ones, where the block at (row0, col0) has them: its row `lane` keeps their unit at `unit` of shared memory.
+template <typename T>
+__device__ __forceinline__ void store_rest(void* out, const GemmArgs& p, uint32_t unit, int row0, int lane)
+{
+    constexpr int V = Pack<T>::V, E = (int)sizeof(T);
+    if (row0 + lane >= p.rows) return;
+    const int whole = whole_columns<T>(p.cols);
+    typename Pack<T>::Word* q = reinterpret_cast<typename Pack<T>::Word*>(out) + (int64_t)(row0 + lane) * p.ld + whole;
+#pragma unroll
+    for (int j = 0; j < V - 1; ++j)
+        if (whole + j < p.cols) q[j] = Pack<T>::shared_word(unit + j * E);
+}
 // A 32 x 32 block on its way out by a tensor copy: a lane holds row `lane`; 16-byte units are spread as the copy's swizzle has them.
 template <typename T>
 struct Slab {
     static constexpr int kBytes = 32 * 32 * sizeof(T), kSlabs = kBlock / kBytes;
+    static __device__ __forceinline__ uint32_t at(uint32_t slab, int lane, int u)
+    {
+        return sizeof(T) == 2 ? slab + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4) : slab + lane * 128 + ((u ^ (lane & 7)) << 4);
+    }
     static __device__ __forceinline__ void put(uint32_t slab, int lane, const float* v)
     {
         constexpr int V = Pack<T>::V;
 #pragma unroll
         for (int u = 0; u < 32 / V; ++u) {
-            const uint32_t at = sizeof(T) == 2 ? slab + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4) : slab + lane * 128 + ((u ^ (lane & 7)) << 4);
             const uint4 w = Pack<T>::pack(v + u * V);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at(slab, lane, u)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
         }
     }
 };
-// One warp sends the block of out at (row0, col0) off, `n` counting its copies.  Rows and columns beyond out are cut off by the copy.
+// One warp sends the block of out at (row0, col0) off, `n` counting its copies.  Rows and whole units beyond out are cut off by the copy.
 template <typename T>
-__device__ __forceinline__ void send_slab(const CUtensorMap* map, uint32_t slabs, int* n, const float* v, int row0, int col0, int lane)
+__device__ __forceinline__ void send_slab(const CUtensorMap* map, void* out, const GemmArgs& p, uint32_t slabs, int* n, const float* v, int row0, int col0, int lane)
 {
+    const int whole = whole_columns<T>(p.cols);
     const uint32_t slab = slabs + (*n % Slab<T>::kSlabs) * Slab<T>::kBytes;
     ++*n;
     if (lane == 0) tma_store_wait<Slab<T>::kSlabs - 1>();
     __syncwarp();
     Slab<T>::put(slab, lane, v);
+    if (whole < p.cols && col0 + 32 > whole) store_rest<T>(out, p, Slab<T>::at(slab, lane, (whole - col0) / Pack<T>::V), row0, lane);
     fence_async_smem();
     __syncwarp();
-    if (lane == 0) tma_store_2d(map, slab, col0, row0);
+    if (lane == 0 && col0 < whole) tma_store_2d(map, slab, col0, row0);
 }
 // Two blocks side by side as one copy of 64 columns of a 16-bit type, the left one first: what a copy out takes goes with its rows (about 7 clocks of
 // the copy engine each), not with their length.  (4096 x 4096 gradients of 128 rows: 12.5 us with copies of 32 columns.)
 template <typename T>
-__device__ __forceinline__ void send_half(const CUtensorMap* map, uint32_t slab, const float* v, int row0, int col0, int cols, int lane)
+__device__ __forceinline__ void send_half(const GemmArgs& p, uint32_t slab, const float* v, int row0, int col0, int lane)
 {
     if constexpr (sizeof(T) == 2) {
+        const int whole = whole_columns<T>(p.cols);
         const int half = (col0 >> 5) & 1;
         if (!half) {
             if (lane == 0) tma_store_wait<0>();
@@ -355,10 +376,11 @@ __device__ __forceinline__ void send_half(const CUtensorMap* map, uint32_t slab,
             const uint4 w = Pack<T>::pack(v + u * 8);
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(unit_at(slab, lane, half * 4 + u)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
         }
-        if (half || col0 + 32 >= cols) {                       // (the right half may lie behind the last column)
+        if (whole < p.cols && col0 + 32 > whole) store_rest<T>(p.out, p, unit_at(slab, lane, half * 4 + (whole - col0) / Pack<T>::V), row0, lane);
+        if (half || col0 + 32 >= p.cols) {                     // (the right half may lie behind the last column)
             fence_async_smem();
             __syncwarp();
-            if (lane == 0) tma_store_2d(map, slab, col0 - half * 32, row0);
+            if (lane == 0 && col0 - half * 32 < whole) tma_store_2d(&p.t_out, slab, col0 - half * 32, row0);
         }
     }
 }
@@ -426,7 +448,7 @@ __device__ __forceinline__ void send_block(const GemmArgs& p, uint32_t slabs, ui
         }
     }
     if (p.z) {
-        if (p.copy_out) send_slab<T>(&p.t_z, slabs, n, v, row0, col0, lane);
+        if (p.copy_out) send_slab<T>(&p.t_z, p.z, p, slabs, n, v, row0, col0, lane);
         else store_slab<T>(p.z, p, slabs, v, row0, col0, lane);
     }
     if (p.act != HPF_ACT_NONE) activate<32>(v, p.act);
@@ -439,8 +461,8 @@ __device__ __forceinline__ void send_block(const GemmArgs& p, uint32_t slabs, ui
             for (int j = 0; j < V; ++j) v[u * V + j] += f[j];
         }
     }
-    if (p.copy_out == 64) send_half<T>(&p.t_out, slabs, v, row0, col0, p.cols, lane);
-    else if (p.copy_out) send_slab<T>(&p.t_out, slabs, n, v, row0, col0, lane);
+    if (p.copy_out == 64) send_half<T>(p, slabs, v, row0, col0, lane);
+    else if (p.copy_out) send_slab<T>(&p.t_out, p.out, p, slabs, n, v, row0, col0, lane);
     else store_slab<T>(p.out, p, slabs, v, row0, col0, lane);
 }
 
@@ -1084,11 +1106,11 @@ cudaError_t make_map(CUtensorMap* tm, const Operand& o, int32_t dtype, int box_r
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
-// map of an output: copies of 32 rows x 32 or 64 columns
+// map of an output: copies of 32 rows x 32 or 64 columns, of the row's whole 16-byte units (see store_rest)
 template <typename T>
 cudaError_t make_out_map(CUtensorMap* tm, void* out, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, int width)
 {
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t dims[2] = {(cuuint64_t)(cols & -(int64_t)(16 / sizeof(T))), (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)(ld * sizeof(T))};
     const cuuint32_t box[2] = {(cuuint32_t)width, 32};
     const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == HPF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
@@ -1166,7 +1188,7 @@ template <int E, typename T, bool PROMOTE>
 cudaError_t launch_width(GemmArgs& g, int bn, int32_t dtype, cudaStream_t st)
 {
     // 64 columns where one warp has two blocks side by side and its staging is needed for one output only
-    g.copy_out = !g.wide || g.split > 1 || g.swap ? 0 : sizeof(T) == 2 && bn >= 128 && !g.z ? 64 : 32;
+    g.copy_out = !g.wide || g.split > 1 || g.swap || g.cols < 16 / (int)sizeof(T) ? 0 : sizeof(T) == 2 && bn >= 128 && !g.z ? 64 : 32;
     if (g.copy_out) {
         cudaError_t e = make_out_map<T>(&g.t_out, g.out, g.rows, g.cols, g.ld, dtype, g.copy_out);
         if (e == cudaSuccess && g.z) e = make_out_map<T>(&g.t_z, g.z, g.rows, g.cols, g.ld, dtype, g.copy_out);
