@@ -12,7 +12,8 @@
 // warps write lo beside each stage and three MMAs form hi hi + lo hi + hi lo.  What is left out of a product (lo lo, and the bits of a lo
 // that TF32 drops) is below 3 2^-20 of it, about 2^-21 on average.
 // The accumulator truncates each addition, an error that grows with the number of additions and always points to zero: where the
-// result is fp32, sums are taken out of TMEM every few stages and added up in registers, rounded to nearest.
+// result is fp32, sums are taken out of TMEM every few stages and added up in registers, rounded to nearest; where it has 16 bits, every 64
+// stages of a long sum.
 //
 // Few tiles (few rows, small layers): the k loop is split over a cluster of up to 8 CTAs.  Each leaves its fp32 partial tile in
 // its own shared memory; the CTAs then add the partial tiles up over distributed shared memory, always in rank order.
@@ -83,6 +84,18 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v)
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
+// Back to where tmem_ld32 has them, 16 columns; read again after tmem_st_wait()
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v)
+{
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // A wait that does not look at the abort flag: for copies in flight after another wait gave up.
 __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity)
 {
@@ -584,16 +597,23 @@ struct Shape {
     static constexpr int kStages = kRing / kStage < kMaxStages ? kRing / kStage : kMaxStages;
     static constexpr int kThreads = (4 + kOutWarps + (E == 4 ? 4 : 0)) * 32;
     static constexpr int kInner = kRow / E;              // values in a row of a stage
-    // Stages whose products are added up in TMEM where the result is fp32: 12 or 16 truncating additions.  (fp32 operands: with 4
-    // stages, 48 additions, a product of K = 2048 was 1.2e-6 off, with 1 stage it is as far off as one summed in fp32 FMAs.)
-    static constexpr int kChunk = E == 4 ? 1 : 4;
 };
+// Stages whose products are added up in TMEM where sums leave it on the way (PROMOTE).  fp32 results: 12 or 16 truncating additions.  (fp32
+// operands: with 4 stages, 48 additions, a product of K = 2048 was 1.2e-6 off, with 1 stage it is as far off as one summed in fp32 FMAs.)
+// 16-bit results of long sums: 256 additions, each up to a step short and as much inside: at most 2^-14 of the sum, 1 / 8 of half a step of fp16.
+template <int E, typename T>
+constexpr int kChunkStages = E == 4 ? 1 : sizeof(T) == 4 ? 4 : 64;
+// Stages up to which a CTA's sums for 16-bit results stay in TMEM: 512 additions, at most 2^-13 short.  (With no such limit sums of
+// 2^20 products of one sign, 8192 additions a CTA, came out 1.25e-3 too small: 2.5 half steps of fp16.  Taking them out costs nothing that can be
+// measured: 8192 x 16384 -> 4096 bf16 759 us either way.)
+constexpr int kLongSum = 128;
 
 template <int E, typename T, int BN, bool PROMOTE>
 __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(const __grid_constant__ GemmArgs p)
 {
     using S = Shape<E, BN>;
-    constexpr int STAGES = S::kStages;
+    constexpr int STAGES = S::kStages, CHUNK = kChunkStages<E, T>;
+    constexpr bool LONG = PROMOTE && sizeof(T) == 2;        // long sums of 16-bit results: back in TMEM for the write-out
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long s_bars[3 * kMaxStages + 5];
     __shared__ uint32_t s_tmem;
@@ -674,7 +694,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
             bool live = true;
             for (int t = first; live && t < tiles; t += step) {
                 for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int in_chunk = PROMOTE ? (kb - kb0) % S::kChunk : kb - kb0;
+                    const int in_chunk = PROMOTE ? (kb - kb0) % CHUNK : kb - kb0;
                     const int buf = chunk & 1;
                     if (in_chunk == 0) {
                         if (!mbar_wait(acc_empty + 8 * buf, ((chunk >> 1) & 1) ^ 1, abort_flag)) { report(p.status, 41); live = false; break; }
@@ -707,7 +727,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                         }
                     }
                     umma_commit(empty + 8 * s);
-                    if (kb + 1 == kb1 || (PROMOTE && in_chunk + 1 == S::kChunk)) {
+                    if (kb + 1 == kb1 || (PROMOTE && in_chunk + 1 == CHUNK)) {
                         umma_commit(acc_full + 8 * buf);
                         ++chunk;
                     }
@@ -724,7 +744,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
         const uint32_t mine = staging + (warp - 4) * kBlock;
         const uint32_t bias = staging + kOutWarps * kBlock + (warp - 4) * 128;
         float acc[PROMOTE ? BLOCKS : 1][32];
-        int chunk = 0, sent = 0;
+        int chunk = 0, sent = 0, held = 0;                    // held: the accumulator that has the finished sums
         bool live = true;
         for (int t = first; live && t < tiles; t += step) {
             const Tile tile = tile_at(t, p.tiles_m, p.tiles_n);
@@ -741,12 +761,12 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                 finish_rows<T, 32>(p, mine, 1, row0, col0, lane);
                 __syncwarp();
             };
-            if constexpr (PROMOTE) {
+            if constexpr (PROMOTE && !LONG) {
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) acc[b][j] = 0.f;
-                for (int kb = kb0; live && kb < kb1; kb += S::kChunk, ++chunk) {
+                for (int kb = kb0; live && kb < kb1; kb += CHUNK, ++chunk) {
                     const int buf = chunk & 1;
                     live = mbar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, abort_flag);
                     live = __all_sync(0xffffffffu, live);
@@ -771,22 +791,52 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                     for (int b = 0; b < BLOCKS; ++b) hand_over(half * BLOCKS + b, acc[b]);
                 }
             } else {
-                const int buf = chunk & 1;
-                live = mbar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, abort_flag);
-                live = __all_sync(0xffffffffu, live);
-                if (!live) { report(p.status, 43); break; }
-                tc_fence_after();
-                ++chunk;
+                if constexpr (LONG) {
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) acc[b][j] = 0.f;
+                }
+                for (int kb = kb0;; kb += CHUNK) {
+                    held = chunk & 1;
+                    live = mbar_wait(acc_full + 8 * held, (chunk >> 1) & 1, abort_flag);
+                    live = __all_sync(0xffffffffu, live);
+                    if (!live) { report(p.status, 43); break; }
+                    tc_fence_after();
+                    ++chunk;
+                    if constexpr (!LONG) break;
+                    if (BN > 32 || half == 0) {
+#pragma unroll
+                        for (int i = 0; i < 2 * BLOCKS; ++i) {
+                            float v[16], *sums = acc[i >> 1] + (i & 1) * 16;
+                            tmem_ld16(tmem + lanes + held * BN + half * BLOCKS * 32 + i * 16, v);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) sums[j] += v[j];
+                        }
+                    }
+                    if (kb + CHUNK >= kb1) break;
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(acc_empty + 8 * held);
+                }
+                if (!live) break;
+                if constexpr (LONG) {
+                    if (BN > 32 || half == 0) {
+#pragma unroll
+                        for (int i = 0; i < 2 * BLOCKS; ++i) tmem_st16(tmem + lanes + held * BN + half * BLOCKS * 32 + i * 16, acc[i >> 1] + (i & 1) * 16);
+                    }
+                    tmem_st_wait();
+                }
                 if (split > 1) break;                          // the sums are fetched once the whole cluster is done
 #pragma unroll 1
                 for (int b = 0; b < BLOCKS; ++b) {
                     const int c = half * BLOCKS + b;
                     float v[32];
-                    if (BN > 32 || half == 0) tmem_ld32(tmem + lanes + buf * BN + c * 32, v);
+                    if (BN > 32 || half == 0) tmem_ld32(tmem + lanes + held * BN + c * 32, v);
                     if (b == BLOCKS - 1) {
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
+                        if (lane == 0) mbar_arrive(acc_empty + 8 * held);
                     }
                     if (BN > 32 || half == 0) hand_over(c, v);
                 }
@@ -804,9 +854,9 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
                 for (int b = 0; b < BLOCKS; ++b) {
                     const int c = half * BLOCKS + b;
                     float v[32];
-                    if constexpr (!PROMOTE) tmem_ld32(tmem + lanes + c * 32, v);
+                    if constexpr (!PROMOTE || LONG) tmem_ld32(tmem + lanes + held * BN + c * 32, v);
                     const float* sums = v;
-                    if constexpr (PROMOTE) sums = acc[b];
+                    if constexpr (PROMOTE && !LONG) sums = acc[b];
                     block_put(ring + (c * 4 + quad) * kBlock, lane, sums, p.swap);
                 }
                 fence_async_smem();
@@ -1194,7 +1244,7 @@ cudaError_t launch_width(GemmArgs& g, int bn, int32_t dtype, cudaStream_t st)
         if (e == cudaSuccess && g.z) e = make_out_map<T>(&g.t_z, g.z, g.rows, g.cols, g.ld, dtype, g.copy_out);
         if (e != cudaSuccess) return e;
     }
-    if constexpr (!PROMOTE) {
+    if constexpr (sizeof(T) == 2) {
         if (bn == 256) return launch_gemm<E, T, 256, PROMOTE>(g, st);
     }
     return bn == 128 ? launch_gemm<E, T, 128, PROMOTE>(g, st) : bn == 64 ? launch_gemm<E, T, 64, PROMOTE>(g, st) : launch_gemm<E, T, 32, PROMOTE>(g, st);
@@ -1238,6 +1288,8 @@ cudaError_t gemm(GemmArgs& g, Operand a, Operand b, int64_t rows, int64_t cols, 
         return launch_width<4, float, true>(g, plan.bn, dtype, st);
     } else {
         if (out_fp32) return launch_width<2, float, true>(g, plan.bn, dtype, st);
+        if ((g.k_blocks + g.split - 1) / g.split > kLongSum)
+            return dtype == HPF_BF16 ? launch_width<2, __nv_bfloat16, true>(g, plan.bn, dtype, st) : launch_width<2, __half, true>(g, plan.bn, dtype, st);
         return dtype == HPF_BF16 ? launch_width<2, __nv_bfloat16, false>(g, plan.bn, dtype, st) : launch_width<2, __half, false>(g, plan.bn, dtype, st);
     }
 }
