@@ -359,7 +359,7 @@ int hpf_sgd_momentum_flat(const float *d_slots, float *d_grad_avg, float *d_para
  * computed with in fp32.  A logit of -inf is a masked class: it has probability 0, is never listed and gets gradient 0.
  * A row with nothing but -inf has no distribution (see each call).  A row with a NaN or +inf gives NaN.  A label
  * outside [0, classes) is no label.  Statistics, losses and lists are fp32 / int32.  No workspace; temperatures lie in
- * [1e-30, 1e30]; a call is one kernel on `stream` of the current device, may be captured, and rows = 0 does nothing.  Results do not depend on timing. */
+ * [1e-30, 1e30] (distillation: [0.001, 100]); a call is one kernel on `stream` of the current device, may be captured, and rows = 0 does nothing.  Results do not depend on timing. */
 typedef enum { HPF_FP32 = 0, HPF_BF16 = 1, HPF_FP16 = 2 } hpf_dtype;
 
 /* The linear layer  z = x W^T + bias,  y = act(z) + residual:  d_x [rows][n_in] (rows ld_x elements apart), d_w [n_out][n_in],
@@ -367,7 +367,8 @@ typedef enum { HPF_FP32 = 0, HPF_BF16 = 1, HPF_FP16 = 2 } hpf_dtype;
  * the backward call needs it (any activation but NONE), else NULL.  All of type dtype, sums in fp32 (for 16-bit results
  * short by at most 2^-13 of their largest partial sum, however long they are); fp32 tensors go through the
  * tensor cores as three TF32 products per term (each within 3 2^-20; an infinity in x or W gives NaN).  GELU is z Phi(z), SILU z / (1 + e^-z), of
- * fp32 within a relative 2^-19 + 1.5 z^2 2^-24 wherever the result is not below fp32's normal values, of 16-bit types exact but for the last rounding.
+ * fp32 within a relative 2^-19 + 1.5 z^2 2^-24 wherever the result is not below fp32's normal values, of 16-bit types within
+ * 2^-15 + 1.5 z^2 2^-24 and the last rounding.
  * No output may overlap an input but as said.  Any sizes, strides and alignments that the type has; rows that do not start on 16-byte boundaries cost a copy in scratch.
  * d_scratch: 16-byte aligned, scratch_bytes of it as hpf_linear_scratch_bytes says (aligned = 0: for tensors whose first element
  * is not on a 16-byte boundary); its first 8 bytes are zeroed once by the caller and tell hpf_linear_status whether a bounded wait ever
@@ -407,7 +408,8 @@ int hpf_logprobs_bwd(const void *d_logits, const int32_t *d_labels, const float 
  *   loss[row] = alpha T^2 sum_j q_j (ln q_j - ln p_T[id_j]) + (1 - alpha) (-ln p[label])
  * Entries outside [0, classes) or at -inf are not there; a list that holds nothing and a missing label drop their term; a class
  * listed twice counts with both weights.  A masked class with q > 0 makes the loss +inf.  A row without a distribution has loss 0.
- * d_labels may be NULL if alpha = 1.  d_stats [rows][2] is what the backward call needs (may be NULL). */
+ * d_labels may be NULL if alpha = 1.  T lies in [0.001, 100]: the logarithms are good to about 1e-6 and their differences carry T^2, so that
+ * the loss is good to about 2e-6 alpha T^2 (the gradient to 1e-6 alpha T max(p_T, q)) and would be noise or overflow further out.  d_stats [rows][2] is what the backward call needs (may be NULL). */
 int hpf_distill_fwd(const void *d_logits, const int32_t *d_labels, const int32_t *d_teacher_ids, const float *d_teacher_logits,
                     float *d_loss, float *d_stats, int64_t rows, int32_t classes, int64_t ld, int32_t k, float temperature,
                     float alpha, int32_t dtype, void *stream);

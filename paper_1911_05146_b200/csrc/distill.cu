@@ -337,7 +337,8 @@ int check_distill(const void* logits, const int32_t* labels, const int32_t* ids,
 {
     const int bad = check_rows(logits, rows, classes, ld, dtype);
     if (bad != HPF_OK) return bad;
-    if (!temperature_ok(temperature)) return api_fail(HPF_ERR_INVALID, "the temperature must lie in [1e-30, 1e30]");
+    // the loss is a difference of logarithms, good to 1e-6, times T^2: beyond 100 that is as large as the loss of a list of all classes, and T^2 overflows in the end
+    if (!(temperature >= 1e-3f && temperature <= 100.f)) return api_fail(HPF_ERR_INVALID, "the temperature of a distillation must lie in [0.001, 100]");
     if (!(alpha >= 0.f && alpha <= 1.f)) return api_fail(HPF_ERR_INVALID, "alpha must lie in [0, 1]");
     if (k < 0 || k > kMaxTeacher) return api_fail(HPF_ERR_UNSUPPORTED, "a teacher's list has at most 256 entries per row");
     if (rows && ((k && (!ids || !teacher)) || (alpha < 1.f && !labels))) return api_fail(HPF_ERR_INVALID, "null list, or null labels with alpha < 1");
