@@ -2,6 +2,7 @@
 import ctypes as C
 import importlib.machinery
 import importlib.util
+import operator
 import os
 
 from . import build as _build
@@ -154,7 +155,17 @@ def _dtype_of(dtype, what):
 
 
 _calls = None
-_CALLS = ("linear_fwd", "linear_bwd", "logprobs_fwd", "logprobs_bwd", "distill_fwd", "distill_bwd", "distill_fwd_bwd")
+# What each call takes: tensors of the call's type (t), of the weight gradients' (g), of labels and classes (i), of statistics (f), scratch (s), and
+# numbers, in the order of the C functions; theirs take the types, scratch's size and the stream besides.
+_CALLS = {
+    "linear_fwd": "x:t w:t bias:t residual:t y:t z:t rows n_in n_out ld_x ld_y :dtype act scratch:s",
+    "linear_bwd": "dy:t z:t x:t w:t dx:t dw:g dbias:g rows n_in n_out ld_x ld_y :dtype act :grad scratch:s",
+    "logprobs_fwd": "logits:t labels:i logprob:f entropy:f lse:f top_ids:i top_logprobs:f rows classes ld k temperature :dtype",
+    "logprobs_bwd": "logits:t labels:i lse:f entropy:f d_logprob:f d_entropy:f d_logits:t rows classes ld ld_d temperature :dtype",
+    "distill_fwd": "logits:t labels:i teacher_ids:i teacher_logits:f loss:f stats:f rows classes ld k temperature alpha :dtype",
+    "distill_bwd": "logits:t labels:i teacher_ids:i teacher_logits:f stats:f d_loss:f d_logits:t rows classes ld ld_d k temperature alpha :dtype",
+    "distill_fwd_bwd": "logits:t labels:i teacher_ids:i teacher_logits:f d_loss:f loss:f d_logits:t rows classes ld ld_d k temperature alpha :dtype",
+}
 
 
 def _refused(status, what, tensor):
@@ -164,15 +175,71 @@ def _refused(status, what, tensor):
     _check(status)
 
 
+class _CtypesCalls:
+    """The calls of csrc/py_calls.c marshalled by ctypes, for an interpreter that the extension could not be compiled for (6 us a call where it takes 1.7)."""
+
+    def setup(self, refused, get_device, get_stream, types, addresses):
+        self._refused, self._get_device, self._get_stream, self._types = refused, get_device, get_stream, types
+        for name, address in zip(_CALLS, addresses):
+            f = C.CFUNCTYPE(C.c_int, *_SIGNATURES["hpf_" + name])(address)
+            setattr(self, name, lambda *args, f=f, spec=_CALLS[name].split(), kinds=_SIGNATURES["hpf_" + name]: self._call(f, spec, kinds, args))
+
+    def _type_of(self, t, name):
+        if t.dtype not in self._types[:3]:
+            self._refused(ERR_INVALID, name, t)
+        return self._types.index(t.dtype)
+
+    def _call(self, f, spec, kinds, args):
+        names = [s for s in spec if s[0] != ":"]
+        if len(args) != len(names) + 1:
+            raise TypeError(f"{len(names) + 1} arguments are wanted, got {len(args)}")
+        value = dict(zip((s.partition(":")[0] for s in names), args))
+        device, dtype = self._get_device(), self._type_of(args[0], names[0][:-2])
+        grad = dtype
+        for name in ("dw", "dbias"):
+            if value.get(name) is not None:
+                grad = self._type_of(value[name], name)
+                break
+        wanted = {"t": self._types[dtype], "g": self._types[grad], "i": self._types[3], "f": self._types[0], "s": self._types[4]}
+        out = []
+        for s in spec:
+            name, _, kind = s.partition(":")
+            v = value.get(name)
+            if not name:
+                out.append(dtype if kind == "dtype" else grad)
+            elif kind:
+                if v is not None and (v.dtype != wanted[kind] or v.get_device() != device):
+                    self._refused(ERR_INVALID, name, v)
+                out.append(None if v is None else v.data_ptr())
+                if kind == "s":
+                    out.append(0 if v is None else v.numel())
+            elif kinds[len(out)] is _f32:
+                out.append(C.c_float(v).value)
+            else:
+                bits = 8 * C.sizeof(kinds[len(out)])       # (ctypes would cut off what is above)
+                if not -1 << bits - 1 <= operator.index(v) < 1 << bits - 1:
+                    raise OverflowError(f"{name} does not fit {bits} bits")
+                out.append(operator.index(v))
+        stream = args[-1]
+        out.append(self._get_stream(device) if stream is None else stream if isinstance(stream, int) else stream.cuda_stream)
+        status = f(*out)
+        if status:
+            self._refused(status, "", None)
+
+
 def _fast():
-    """The calls of py_calls.c, with the library's addresses and torch's types."""
+    """The calls of py_calls.c (by ctypes where it could not be compiled), with the library's addresses and torch's types."""
     global _calls
     if _calls is None:
         import torch
         L = lib()
-        loader = importlib.machinery.ExtensionFileLoader("_calls", _build.CALLS)
-        m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
-        loader.exec_module(m)
+        path = _build.calls()
+        if path:
+            loader = importlib.machinery.ExtensionFileLoader("_calls", path)
+            m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_calls", loader))
+            loader.exec_module(m)
+        else:
+            m = _CtypesCalls()
         torch.cuda.init()
         m.setup(_refused, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, (torch.float32, torch.bfloat16, torch.float16, torch.int32, torch.uint8),
                 tuple(C.cast(getattr(L, "hpf_" + n), _vp).value for n in _CALLS))
