@@ -368,7 +368,7 @@ typedef enum { HPF_FP32 = 0, HPF_BF16 = 1, HPF_FP16 = 2 } hpf_dtype;
  * short by at most 2^-13 of their largest partial sum, however long they are); fp32 tensors go through the
  * tensor cores as three TF32 products per term (each within 3 2^-20; an infinity in x or W gives NaN).  GELU is z Phi(z), SILU z / (1 + e^-z), of
  * fp32 within a relative 2^-19 + 1.5 z^2 2^-24 wherever the result is not below fp32's normal values, of 16-bit types within
- * 2^-15 + 1.5 z^2 2^-24 and the last rounding.
+ * 2^-18 + 1.5 z^2 2^-24 and the last rounding.
  * No output may overlap an input but as said.  Any sizes, strides and alignments that the type has; rows that do not start on 16-byte boundaries cost a copy in scratch.
  * d_scratch: 16-byte aligned, scratch_bytes of it as hpf_linear_scratch_bytes says (aligned = 0: for tensors whose first element
  * is not on a 16-byte boundary); its first 8 bytes are zeroed once by the caller and tell hpf_linear_status whether a bounded wait ever

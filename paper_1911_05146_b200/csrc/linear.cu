@@ -53,6 +53,7 @@ struct GemmArgs {
     uint32_t idesc;
     int act, wide;                             // wide: every output and the residual take 16-byte accesses
     int copy_out;                              // tiles leave by tensor copies (wide, whole k in one CTA, rows of out in the lanes) of so many columns
+    int by_slab;                               // by these, or column by column through the same blocks; else row by row (finish_rows)
     void *out, *z;
     const void *bias, *residual;
     int64_t ld;                                // of out, z and residual
@@ -186,21 +187,22 @@ __device__ __forceinline__ float reciprocal(float x)
 __device__ __forceinline__ f2 both(float v) { return pair(v, v); }
 // gelu is z Phi(z), its slope Phi(z) + z phi(z).  Phi(-|z|) = Q(t) e^(-z^2 / 2) with t = 1 / (1 + P |z|): Q, half the scaled complementary error function,
 // is smooth in t and was fitted with the least largest relative error over |z| <= 14.5, where e^(-z^2 / 2) leaves fp32.  So the small values of the
-// negative side are as exact as the large ones.  Six terms: 9.2e-6, a fiftieth of half a step of fp16; nine, for fp32: 6.4e-8.  e^(-z^2 / 2) is what phi
-// needs too: 2 special-function results a value where erff and expf took about 60 instructions (the dz kernel of 8192 x 16384 bf16: 354 us with those).
+// negative side are as exact as the large ones.  Seven terms: 1.5e-6; nine, for fp32: 6.4e-8 (a layer of 8192 x 64 -> 16384 bf16, all write-out: 143 us with nine,
+// 136 with seven, 134 with five, which get 5.6e-5).  e^(-z^2 / 2) is what phi needs too: 2 special-function results a value where erff and expf took about 60
+// instructions (the dz kernel of 8192 x 16384 bf16: 354 us with those).
 template <typename T> struct Tail {
-    static constexpr int N = 6;
-    static constexpr float P = 0.318198052f;
-    static __device__ __forceinline__ float q(int i)
+    static constexpr int N = 7;
+    static constexpr float P = 0.353553391f;
+    static __device__ __forceinline__ float term(int i)
     {
-        const float c[N] = {0.126960934f, 0.126086997f, 0.123348771f, 0.0463016689f, 0.14480765f, -0.0675105839f};
+        const float c[N] = {0.141161801f, 0.138845259f, 0.14046068f, 0.0197253018f, 0.193506594f, -0.17757707f, 0.043876714f};
         return c[i];
     }
 };
 template <> struct Tail<float> {
     static constexpr int N = 9;
     static constexpr float P = 0.282842712f;
-    static __device__ __forceinline__ float q(int i)
+    static __device__ __forceinline__ float term(int i)
     {
         const float c[N] = {0.112818819f, 0.11319271f, 0.101148179f, 0.0959035988f, 0.0417257859f, 0.0413279856f, 0.0442964147f, -0.0712659048f, 0.0208524438f};
         return c[i];
@@ -216,9 +218,9 @@ __device__ __forceinline__ void gauss(f2 z, f2* cdf, f2* e)
     split(fma2(pair(fabsf(z0), fabsf(z1)), both(Tail<T>::P), both(1.f)), &d0, &d1);
     const f2 t = pair(reciprocal(d0), reciprocal(d1));
     *e = ex2_2(mul2(mul2(z, z), both(-0.72134752044f)));
-    f2 q = both(Tail<T>::q(N - 1));
+    f2 q = both(Tail<T>::term(N - 1));
 #pragma unroll
-    for (int i = N - 2; i >= 0; --i) q = fma2(t, q, both(Tail<T>::q(i)));
+    for (int i = N - 2; i >= 0; --i) q = fma2(t, q, both(Tail<T>::term(i)));
     const f2 tail = mul2(mul2(t, q), *e);
     float t0, t1, u0, u1;
     split(tail, &t0, &t1);
@@ -344,61 +346,40 @@ __device__ __forceinline__ void tma_store_wait()
 {
     asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
 }
-// A copy out writes whole 16-byte units, also past the last column of its tensor: what of a row's last unit is in `out` is left to the lanes.
-template <typename T>
-__device__ __forceinline__ int whole_columns(int cols) { return cols & -Pack<T>::V; }
-// The columns behind the whole ones, where the block at (row0, col0) has them: its row `lane` keeps their unit at `unit` of shared memory.
-template <typename T>
-__device__ __forceinline__ void store_rest(void* out, const GemmArgs& p, uint32_t unit, int row0, int lane)
-{
-    constexpr int V = Pack<T>::V, E = (int)sizeof(T);
-    if (row0 + lane >= p.rows) return;
-    const int whole = whole_columns<T>(p.cols);
-    typename Pack<T>::Word* q = reinterpret_cast<typename Pack<T>::Word*>(out) + (int64_t)(row0 + lane) * p.ld + whole;
-#pragma unroll
-    for (int j = 0; j < V - 1; ++j)
-        if (whole + j < p.cols) q[j] = Pack<T>::shared_word(unit + j * E);
-}
 // A 32 x 32 block on its way out by a tensor copy: a lane holds row `lane`; 16-byte units are spread as the copy's swizzle has them.
 template <typename T>
 struct Slab {
     static constexpr int kBytes = 32 * 32 * sizeof(T), kSlabs = kBlock / kBytes;
-    static __device__ __forceinline__ uint32_t at(uint32_t slab, int lane, int u)
-    {
-        return sizeof(T) == 2 ? slab + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4) : slab + lane * 128 + ((u ^ (lane & 7)) << 4);
-    }
     static __device__ __forceinline__ void put(uint32_t slab, int lane, const float* v)
     {
         constexpr int V = Pack<T>::V;
 #pragma unroll
         for (int u = 0; u < 32 / V; ++u) {
+            const uint32_t at = sizeof(T) == 2 ? slab + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4) : slab + lane * 128 + ((u ^ (lane & 7)) << 4);
             const uint4 w = Pack<T>::pack(v + u * V);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at(slab, lane, u)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
         }
     }
 };
-// One warp sends the block of out at (row0, col0) off, `n` counting its copies.  Rows and whole units beyond out are cut off by the copy.
+// One warp sends the block of out at (row0, col0) off, `n` counting its copies.  Rows and columns beyond out are cut off by the copy.
 template <typename T>
-__device__ __forceinline__ void send_slab(const CUtensorMap* map, void* out, const GemmArgs& p, uint32_t slabs, int* n, const float* v, int row0, int col0, int lane)
+__device__ __forceinline__ void send_slab(const CUtensorMap* map, uint32_t slabs, int* n, const float* v, int row0, int col0, int lane)
 {
-    const int whole = whole_columns<T>(p.cols);
     const uint32_t slab = slabs + (*n % Slab<T>::kSlabs) * Slab<T>::kBytes;
     ++*n;
     if (lane == 0) tma_store_wait<Slab<T>::kSlabs - 1>();
     __syncwarp();
     Slab<T>::put(slab, lane, v);
-    if (whole < p.cols && col0 + 32 > whole) store_rest<T>(out, p, Slab<T>::at(slab, lane, (whole - col0) / Pack<T>::V), row0, lane);
     fence_async_smem();
     __syncwarp();
-    if (lane == 0 && col0 < whole) tma_store_2d(map, slab, col0, row0);
+    if (lane == 0) tma_store_2d(map, slab, col0, row0);
 }
 // Two blocks side by side as one copy of 64 columns of a 16-bit type, the left one first: what a copy out takes goes with its rows (about 7 clocks of
 // the copy engine each), not with their length.  (4096 x 4096 gradients of 128 rows: 12.5 us with copies of 32 columns.)
 template <typename T>
-__device__ __forceinline__ void send_half(const GemmArgs& p, uint32_t slab, const float* v, int row0, int col0, int lane)
+__device__ __forceinline__ void send_half(const CUtensorMap* map, uint32_t slab, const float* v, int row0, int col0, int cols, int lane)
 {
     if constexpr (sizeof(T) == 2) {
-        const int whole = whole_columns<T>(p.cols);
         const int half = (col0 >> 5) & 1;
         if (!half) {
             if (lane == 0) tma_store_wait<0>();
@@ -409,11 +390,10 @@ __device__ __forceinline__ void send_half(const GemmArgs& p, uint32_t slab, cons
             const uint4 w = Pack<T>::pack(v + u * 8);
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(unit_at(slab, lane, half * 4 + u)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
         }
-        if (whole < p.cols && col0 + 32 > whole) store_rest<T>(p.out, p, unit_at(slab, lane, half * 4 + (whole - col0) / Pack<T>::V), row0, lane);
-        if (half || col0 + 32 >= p.cols) {                     // (the right half may lie behind the last column)
+        if (half || col0 + 32 >= cols) {                       // (the right half may lie behind the last column)
             fence_async_smem();
             __syncwarp();
-            if (lane == 0 && col0 - half * 32 < whole) tma_store_2d(&p.t_out, slab, col0 - half * 32, row0);
+            if (lane == 0) tma_store_2d(map, slab, col0 - half * 32, row0);
         }
     }
 }
@@ -481,7 +461,7 @@ __device__ __forceinline__ void send_block(const GemmArgs& p, uint32_t slabs, ui
         }
     }
     if (p.z) {
-        if (p.copy_out) send_slab<T>(&p.t_z, p.z, p, slabs, n, v, row0, col0, lane);
+        if (p.copy_out) send_slab<T>(&p.t_z, slabs, n, v, row0, col0, lane);
         else store_slab<T>(p.z, p, slabs, v, row0, col0, lane);
     }
     if (p.act != HPF_ACT_NONE) activate<T, 32>(v, p.act);
@@ -494,8 +474,8 @@ __device__ __forceinline__ void send_block(const GemmArgs& p, uint32_t slabs, ui
             for (int j = 0; j < V; ++j) v[u * V + j] += f[j];
         }
     }
-    if (p.copy_out == 64) send_half<T>(p, slabs, v, row0, col0, lane);
-    else if (p.copy_out) send_slab<T>(&p.t_out, p.out, p, slabs, n, v, row0, col0, lane);
+    if (p.copy_out == 64) send_half<T>(&p.t_out, slabs, v, row0, col0, p.cols, lane);
+    else if (p.copy_out) send_slab<T>(&p.t_out, slabs, n, v, row0, col0, lane);
     else store_slab<T>(p.out, p, slabs, v, row0, col0, lane);
 }
 
@@ -772,7 +752,7 @@ __global__ void __launch_bounds__(Shape<E, BN>::kThreads, 1) linear_gemm_kernel(
             const auto hand_over = [&](int c, float* v) {
                 const int at_m = tile.m * kTileM + quad * 32, at_n = tile.n * BN + c * 32;
                 const int row0 = p.swap ? at_n : at_m, col0 = p.swap ? at_m : at_n;
-                if (p.copy_out || (!p.swap && !p.residual)) {
+                if (p.by_slab) {
                     send_block<T>(p, mine, bias, &sent, v, at_m, at_n, lane);
                     return;
                 }
@@ -1176,11 +1156,11 @@ cudaError_t make_map(CUtensorMap* tm, const Operand& o, int32_t dtype, int box_r
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
-// map of an output: copies of 32 rows x 32 or 64 columns, of the row's whole 16-byte units (see store_rest)
+// map of an output: copies of 32 rows x 32 or 64 columns
 template <typename T>
 cudaError_t make_out_map(CUtensorMap* tm, void* out, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, int width)
 {
-    const cuuint64_t dims[2] = {(cuuint64_t)(cols & -(int64_t)(16 / sizeof(T))), (cuuint64_t)rows};
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)(ld * sizeof(T))};
     const cuuint32_t box[2] = {(cuuint32_t)width, 32};
     const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == HPF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
@@ -1257,8 +1237,10 @@ Plan choose(int64_t lanes, int64_t cols, int k_blocks, int narrowest, int widest
 template <int E, typename T, bool PROMOTE>
 cudaError_t launch_width(GemmArgs& g, int bn, int32_t dtype, cudaStream_t st)
 {
-    // 64 columns where one warp has two blocks side by side and its staging is needed for one output only
-    g.copy_out = !g.wide || g.split > 1 || g.swap || g.cols < 16 / (int)sizeof(T) ? 0 : sizeof(T) == 2 && bn >= 128 && !g.z ? 64 : 32;
+    // 64 columns where one warp has two blocks side by side and its staging is needed for one output only.  A copy writes whole 16-byte units, also past
+    // the last column: rows that end inside one leave row by row.
+    g.copy_out = !g.wide || g.split > 1 || g.swap || g.cols * sizeof(T) % 16 ? 0 : sizeof(T) == 2 && bn >= 128 && !g.z ? 64 : 32;
+    g.by_slab = g.copy_out || (!g.wide && !g.swap && !g.residual);
     if (g.copy_out) {
         cudaError_t e = make_out_map<T>(&g.t_out, g.out, g.rows, g.cols, g.ld, dtype, g.copy_out);
         if (e == cudaSuccess && g.z) e = make_out_map<T>(&g.t_z, g.z, g.rows, g.cols, g.ld, dtype, g.copy_out);
