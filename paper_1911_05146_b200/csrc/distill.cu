@@ -85,10 +85,11 @@ __device__ __forceinline__ float distill_loss(const DistillArgs& p, const Teache
     const float ln_s = logf(st.s);
     float a = 0.f;
     for (int j = lane; j < p.k; j += 32)
-        if (!(t.q[j] == 0.f)) a += t.q[j] * (t.ln_q[j] - ((t.v[j] - st.m) * p.inv_t - ln_s));
+        // T (ln q - ln p_T): the logit's distance is not divided by T, which leaves fp32 for the type's lowest value
+        if (!(t.q[j] == 0.f)) a += t.q[j] * fmaf(p.temp, t.ln_q[j] + ln_s, st.m - t.v[j]);
 #pragma unroll
     for (int d = 16; d; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
-    float loss = p.alpha > 0.f ? p.alpha * p.temp * p.temp * a : 0.f;
+    float loss = p.alpha > 0.f ? p.alpha * p.temp * a : 0.f;
     if (p.alpha < 1.f && label_there) loss -= (1.f - p.alpha) * ((label_v - st.m1) - logf(st.h));
     return loss;
 }
