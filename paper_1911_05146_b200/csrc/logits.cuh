@@ -30,7 +30,7 @@ namespace {
 constexpr int kWarpRow = 1024;     // classes up to which a warp holds a row
 constexpr int kMaxParts = 8;       // CTAs a row is cut into (portable cluster size)
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kFloor = -1e30f;   // stands for -inf where it meets a weight of 0
+constexpr float kFloor = -1e30f;   // stands for less where a class at it weighs nothing (see LogprobsGrad::far)
 constexpr float kGone = -200.f;    // 2 to this is 0 in fp32
 
 __device__ __forceinline__ float ninf() { return __int_as_float(0xff800000); }
@@ -191,8 +191,8 @@ template <bool ENTROPY, bool HARD>
 __device__ __forceinline__ void rescale(Sums& a, float m, float c)
 {
     if (a.m == m) return;
-    const float u = fmaxf(a.m - m, kFloor), r = ex2(u * c);       // a.m may be -inf: everything it weighs is 0
-    if (ENTROPY) a.w = r * fmaf(u, a.s, a.w);
+    const float u = a.m - m, r = ex2(u * c);                      // -inf where a.m is: what weighs nothing is left out, not multiplied
+    if (ENTROPY) a.w = r == 0.f ? 0.f : r * fmaf(u, a.s, a.w);
     a.s *= r;
     if (HARD) a.h *= ex2(u * kLog2e);
     a.m = m;
@@ -204,7 +204,7 @@ __device__ __forceinline__ void add_value(Sums& a, float v, float c, float base)
     const float u = v - base;
     const float e = ex2(u * c);
     a.s += e;
-    if (ENTROPY) a.w = fmaf(e, fmaxf(u, kFloor), a.w);
+    if (ENTROPY) a.w = e == 0.f ? a.w : fmaf(e, u, a.w);          // u may be -inf; a NaN passes
     if (HARD) a.h += ex2(u * kLog2e);
 }
 __device__ __forceinline__ float base_of(float m) { return m == ninf() ? 0.f : m; }
@@ -222,8 +222,7 @@ constexpr int kNoHard = -1, kOwnExp = 0;
 
 // One thread's share of the row.  ENTROPY: -inf is replaced by the type's lowest value (0 (-inf) would be NaN in the weighted sum) as long as
 // that is so far below the largest logit that it weighs 0 too; else (a strip of nothing but such masks, or a temperature of hundreds
-// in fp16) each class is looked at by itself.  v - m overflows only where m > 10^30, where every class but the largest weighs nothing: see
-// write_stats.
+// in fp16), or where v - m could overflow, each class is looked at by itself.
 // between(): what else has to come from memory, asked for while the first pieces are under way.
 template <typename T, int NT, bool ENTROPY, int POWER, typename F>
 __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, const Stretches* st, F&& between)
@@ -235,7 +234,7 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, c
     f2 s2 = 0, w2 = 0, h2 = 0;
     const f2 c2 = pair(c, c), one2 = pair(kLog2e, kLog2e);
     f2 base2 = 0;                                             // -m, twice
-    const auto near = [&](float m) { return ENTROPY && !((Io<T>::kLowest - m) * c < kGone); };
+    const auto near = [&](float m) { return ENTROPY && !((Io<T>::kLowest - m) * c < kGone && m < 1e30f); };
     bool careful = near(0.f);
     int slot = 0, left = st ? st->iters : 0;
     float stretch = ninf();
@@ -252,9 +251,9 @@ __device__ __forceinline__ Sums run_over(const Share<T>& sh, float c, int tid, c
             }
         }
         if (top > a.m) {
-            const float u = fmaxf(a.m - top, kFloor), r = ex2(u * c);
+            const float u = a.m - top, r = ex2(u * c);            // as in rescale
             const f2 r2 = pair(r, r);
-            if (ENTROPY) w2 = mul2(r2, fma2(pair(u, u), s2, w2));
+            if (ENTROPY) w2 = r == 0.f ? 0 : mul2(r2, fma2(pair(u, u), s2, w2));
             s2 = mul2(r2, s2);
             if (POWER == kOwnExp || POWER > 1) {
                 const float q = ex2(u * kLog2e);
@@ -409,7 +408,7 @@ constexpr float kLseExact = 128.f;   // an lse below this is off by 128 2^-24 = 
 
 // ---- gradients -------------------------------------------------------------------------------------------------------
 // Writes g(two logits) for every two classes of the share.  `out` may be the logits themselves: a thread writes what it has read.
-// BOUNDED: nothing below -10^30 comes.  AGAIN: the row has been gone over just now; it is read from its end to its start, what is in L2
+// BOUNDED: nothing below Io<T>::kBound comes.  AGAIN: the row has been gone over just now; it is read from its end to its start, what is in L2
 // since last first (4096 x 128000 bf16: 487 -> 452 us).
 template <typename T, int NT, bool BOUNDED, bool AGAIN, typename F>
 __device__ __forceinline__ void write_row(const Share<T>& sh, T* out, int tid, F&& g)
@@ -471,7 +470,7 @@ __device__ __forceinline__ void write_row(const Share<T>& sh, T* out, int tid, F
     if (e >= 0) {
         const float v = Io<T>::get(sh.row[e]);
         float a, b;
-        split(g(pair(BOUNDED && v < kFloor ? kFloor : v, 0.f)), &a, &b);
+        split(g(pair(BOUNDED && v < Io<T>::kBound ? Io<T>::kBound : v, 0.f)), &a, &b);
         out[e] = Io<T>::put(a);
     }
 }
