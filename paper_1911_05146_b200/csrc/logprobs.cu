@@ -428,11 +428,11 @@ struct RowScale {
 };
 __device__ __forceinline__ RowScale scale_of(const Sums& a) { return RowScale{base_of(a.m), a.s, a.m == ninf() && a.s == 0.f}; }
 
-struct LogprobsGrad {                // of one row: a class gets p (a + b log2(p S)), the label g on top
-    float c, m, a, b, g_lp, g_h, h, inv_t;
+struct LogprobsGrad {                // of one row: a class gets p (a + b k (v - m)), the label g on top
+    float c, m, a, b, k, g_lp, g_h, h, inv_t;
     int label;
     bool dead;                       // nothing flows back: zeros, whatever the logits hold
-    bool far;                        // scales at which a class at `bound` (what stands for less) would weigh something, or its exponent or that's product with b overflow
+    bool far;                        // scales at which a class at `bound` (what stands for less) would weigh something, or its product with b overflow; `k` other than 1
     __device__ __forceinline__ LogprobsGrad(const LogprobsGradArgs& p, int64_t row)
     {
         label = p.labels ? p.labels[row] : -1;
@@ -448,21 +448,23 @@ struct LogprobsGrad {                // of one row: a class gets p (a + b log2(p
     {
         if (s.none) dead = true;
         m = s.m;
-        // ln p = ln 2 (v - m) c - ln S:  -(g_lp + g_h (ln p + H)) / T.  (1 / T^2 is not formed: it leaves fp32 at either end of the temperatures.)
-        const float w = inv_t / s.s, least = (bound - m) * c;
+        // ln p = (v - m) / T - ln S:  -(g_lp + g_h (ln p + H)) / T.  b k = -w g_h / T; where 1 / T^2 comes near fp32's ends, k takes 1 / T.
+        const float w = inv_t / s.s;
+        const bool apart = !(inv_t > 1e-15f && inv_t < 1e15f);
         a = -w * (g_lp + g_h * (h - logf(s.s)));
-        b = -w * g_h * 0.69314718056f;
-        far = !(fabsf(m) < 1e29f) || !(least < kGone) || !(least * fabsf(b) > -1e37f);
+        b = apart ? -w * g_h : -w * g_h * inv_t;
+        k = apart ? inv_t : 1.f;
+        far = apart || !(fabsf(m) < 1e29f) || !(fabsf(b) < 1e6f) || !((bound - m) * c < kGone);
     }
     __device__ __forceinline__ float slow(float v) const
     {
-        const float u = (v - m) * c, e = ex2(u);
-        return e * (e == 0.f ? a : fmaf(b, u, a));           // (a NaN, of a row without a finite sum, passes)
+        const float u = v - m, e = ex2(u * c);
+        return e * (e == 0.f ? a : fmaf(b, u * k, a));           // (a NaN, of a row without a finite sum, passes)
     }
     __device__ __forceinline__ f2 operator()(f2 v) const
     {
-        const f2 u = mul2(add2(v, pair(-m, -m)), pair(c, c));
-        return mul2(ex2_2(u), fma2(pair(b, b), u, pair(a, a)));
+        const f2 u = add2(v, pair(-m, -m));
+        return mul2(ex2_2(mul2(u, pair(c, c))), fma2(pair(b, b), u, pair(a, a)));
     }
     __device__ __forceinline__ float label_value(float v) const { return slow(v) + g_lp * inv_t; }
 };
