@@ -356,7 +356,8 @@ int hpf_sgd_momentum_flat(const float *d_slots, float *d_grad_avg, float *d_para
 
 /* ---- From features to a loss: the linear layer, log-probabilities, distillation -----------------------------------
  * Logits: d_logits [rows][classes] of type dtype, rows `ld` elements apart (any alignment the type has); 16-bit types are
- * computed with in fp32.  A logit of -inf is a masked class: it has probability 0, is never listed and gets gradient 0.
+ * computed with in fp32.  A logit of -inf is a masked class: it has probability 0 and is never listed, and no part of a
+ * gradient that is a probability's reaches it (what a label or a teacher's class gets besides, it gets masked too).
  * A row with nothing but -inf has no distribution (see each call).  A row with a NaN or +inf gives NaN.  A label
  * outside [0, classes) is no label.  Statistics, losses and lists are fp32 / int32.  No workspace; temperatures lie in
  * [1e-30, 1e30] (distillation: [0.001, 100]); a call is one kernel on `stream` of the current device, may be captured, and rows = 0 does nothing.  Results do not depend on timing. */
@@ -397,7 +398,8 @@ int hpf_logprobs_fwd(const void *d_logits, const int32_t *d_labels, float *d_log
                      int32_t *d_top_ids, float *d_top_logprobs, int64_t rows, int32_t classes, int64_t ld, int32_t k,
                      float temperature, int32_t dtype, void *stream);
 /* d_dlogits = (g (1[class = label] - p) - e p (ln p + entropy)) / temperature with g = d_dlogprob[row] (0 without a label),
- * e = d_dentropy[row] (either may be NULL), lse and entropy as the forward call left them.  Rows with g = e = 0 and rows without a
+ * e = d_dentropy[row] (either may be NULL), lse and entropy as the forward call left them (p is
+ * good to 2^-24 |lse| up to 128; beyond that the sums are formed again).  Rows with g = e = 0 and rows without a
  * distribution get zeros, whatever they hold.  d_dlogits may be d_logits (with ld_d = ld). */
 int hpf_logprobs_bwd(const void *d_logits, const int32_t *d_labels, const float *d_lse, const float *d_entropy,
                      const float *d_dlogprob, const float *d_dentropy, void *d_dlogits, int64_t rows, int32_t classes,
