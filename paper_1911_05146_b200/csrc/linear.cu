@@ -968,12 +968,17 @@ struct Piece {
 
 // A CTA goes down 128 bytes of columns, 32 rows at a time; `parts` CTAs of a cluster share the rows and add their sums up in rank order.
 // The loads of U rows a thread are issued before the first is used.
-template <typename T, bool SHIFT, bool ACT>
+// LONG: blocks of 64 rows a thread are added up by themselves, since a sum of equal values drifts with the additions in a row (2^20 rows of 0.1 came
+// out 3.9e-5 off).  Its registers cost a kernel with an activation 14 %: it is for threads of more than kLongColumn rows.
+constexpr int kLongColumn = 512;
+template <typename T, bool SHIFT, bool ACT, bool LONG>
 __global__ void __launch_bounds__(256, SHIFT ? 3 : 4) linear_dz_kernel(const __grid_constant__ DzArgs p)
 {
     constexpr int COLS = 128 / sizeof(T), V = Pack<T>::V, ROWS = 32, U = ACT || SHIFT ? 2 : 4;
+    constexpr int BLOCK = 64 / U;                            // rounds of a block
     __shared__ float s_sum[8][COLS];
     __shared__ float s_total[COLS];
+    __shared__ float s_block[LONG ? V : 1][LONG ? 256 : 1];  // of the blocks before
     const int part = (int)(blockIdx.x % (unsigned)p.parts);
     const int c0 = (int)(blockIdx.x / (unsigned)p.parts) * COLS;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -991,7 +996,16 @@ __global__ void __launch_bounds__(256, SHIFT ? 3 : 4) linear_dz_kernel(const __g
     dy += first * p.ld;
     z += first * p.ld;
     dz += first * p.ld_dz;
+    int rounds = 0;
     for (int64_t r0 = first; r0 < p.rows; r0 += U * step) {
+        if (LONG && rounds++ % BLOCK == 0 && rounds > 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float& block = s_block[LONG ? j : 0][LONG ? threadIdx.x : 0];
+                block = rounds > BLOCK + 1 ? block + sum[j] : sum[j];
+                sum[j] = 0.f;
+            }
+        }
         Piece<SHIFT> gp[U], zp[ACT ? U : 1];
         uint32_t whole = 0;
 #pragma unroll
@@ -1032,6 +1046,10 @@ __global__ void __launch_bounds__(256, SHIFT ? 3 : 4) linear_dz_kernel(const __g
         dz += U * step * p.ld_dz;
     }
     if (!p.db) return;
+    if (LONG && rounds > BLOCK) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += s_block[LONG ? j : 0][LONG ? threadIdx.x : 0];
+    }
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 8);
@@ -1322,8 +1340,11 @@ cudaError_t launch_dz(DzArgs& a, cudaStream_t st)
     const int64_t want = (a.rows + 255) / 256;
     a.parts = (int)(want > 8 ? 8 : want);
     const bool wide = aligned16(a.dy) && (a.ld * sizeof(T)) % 16 == 0 && (a.act == HPF_ACT_NONE || aligned16(a.z));
-    auto* kernel = a.act == HPF_ACT_NONE ? (wide ? linear_dz_kernel<T, false, false> : linear_dz_kernel<T, true, false>)
-                                         : (wide ? linear_dz_kernel<T, false, true> : linear_dz_kernel<T, true, true>);
+    const bool longer = a.db && a.rows > (int64_t)a.parts * 32 * kLongColumn;
+    auto* kernel = longer ? (a.act == HPF_ACT_NONE ? (wide ? linear_dz_kernel<T, false, false, true> : linear_dz_kernel<T, true, false, true>)
+                                                   : (wide ? linear_dz_kernel<T, false, true, true> : linear_dz_kernel<T, true, true, true>))
+                          : (a.act == HPF_ACT_NONE ? (wide ? linear_dz_kernel<T, false, false, false> : linear_dz_kernel<T, true, false, false>)
+                                                   : (wide ? linear_dz_kernel<T, false, true, false> : linear_dz_kernel<T, true, true, false>));
     return launch(kernel, (unsigned)((a.n + cols - 1) / cols * a.parts), 256, 0, a.parts, st, a);
 }
 
