@@ -530,8 +530,6 @@ cudaError_t launch_warps(K* kernel, int64_t rows, cudaStream_t st, const A& args
 // ---- checks ----------------------------------------------------------------------------------------------------------
 int element(int32_t dtype) { return dtype == HPF_FP32 ? 4 : 2; }
 bool on(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-// 1 / T, and a masked class at the type's lowest value, stay far from the ends of fp32
-bool temperature_ok(float t) { return t >= 1e-30f && t <= 1e30f; }
 int check_rows(const void* logits, int64_t rows, int32_t classes, int64_t ld, int32_t dtype)
 {
     if (dtype != HPF_FP32 && dtype != HPF_BF16 && dtype != HPF_FP16) return api_fail(HPF_ERR_INVALID, "dtype must be HPF_FP32, HPF_BF16 or HPF_FP16");

@@ -567,6 +567,9 @@ cudaError_t logprobs_bwd(LogprobsGradArgs& a, cudaStream_t st)
     return launch_rows(logprobs_bwd_kernel<T, 256>, a.rows, a.parts, 256, st, a, (size_t)a.rows * a.n * sizeof(T));
 }
 
+// 1 / T stays away from the ends of fp32
+bool temperature_ok(float t) { return t >= 1e-30f && t <= 1e30f; }
+
 }  // namespace
 }  // namespace hpf
 
